@@ -66,7 +66,7 @@
  * four-dimensional vectors, d = 4 (the 4D rows of that table): VQ_I8 or VQ_F16, k = 256 (one index
  * byte per 4 weights), groups of 64, 128 or 256 rows x 256 columns (256 rows: 2.125 bits per value
  * with int8 tables, 2.25 with fp16 tables).
- * Every entry point takes all of them.
+ * Every entry point that takes a vq_desc takes all of them.
  */
 #ifndef VQ_H_
 #define VQ_H_
@@ -94,7 +94,7 @@ typedef enum vq_status {
 
 /* VQ_I8 as codebook_dtype: int8 lookup tables with one fp16 scale per group (Sec. 3.1);
  * VQ_I8_BN: the same plus blockwise normalisation (see the canonical format above). */
-typedef enum vq_dtype { VQ_F16 = 1, VQ_F32 = 2, VQ_I8 = 3, VQ_I8_BN = 4 } vq_dtype;
+typedef enum vq_dtype { VQ_F16 = 1, VQ_F32 = 2, VQ_I8 = 3, VQ_I8_BN = 4, VQ_BF16 = 5 /* attention only */ } vq_dtype;
 
 /* Shape of one vector-quantised matrix (Sec. 2.1, Sec. 3.1, Sec. 4). */
 typedef struct vq_desc {
@@ -115,8 +115,9 @@ typedef struct vq_desc {
 /* Human-readable name of a status code (host pointer to a static string). */
 VQ_API const char* vq_status_string(int status);
 
-/* Library version: increments when an entry point is added, a signature or the device layout
- * changes, or a kernel of the decode path is rewritten (measurements quote the version). */
+/* Library version: increments when a signature or the device layout changes, or a kernel of the
+ * weight products is rewritten (their measurements quote the version); entry points that only join
+ * the others leave it as it is. */
 VQ_API int vq_version(void);
 
 /*
@@ -267,6 +268,114 @@ VQ_API int vq_em_assign(const vq_desc* desc, const void* W_f32, const void* hdia
                         const void* cb_f32, void* assign_u8, void* stream);
 VQ_API int vq_em_update(const vq_desc* desc, const void* W_f32, const void* hdiag_f32,
                         const void* assign_u8, void* cb_f32_out, void* stream);
+
+/*
+ * Attention over a paged key-value cache: what stands between the q/k/v products and the o
+ * product of a decoder layer.
+ *
+ * The cache of one layer is a K buffer and a V buffer of n_pages pages each, owned by the caller.
+ * A page holds page_size tokens of every key/value head:
+ *     K  [n_pages][kv_heads][page_size][head_dim]
+ *     V  [n_pages][kv_heads][head_dim][page_size]     (transposed within the page: both products
+ *        of attention run along the contiguous axis of what they read)
+ * Token j of sequence s lies in page page_table[s][j / page_size], slot j % page_size.  Slots that
+ * hold no token may hold anything, NaN and infinities too.
+ *
+ * A call works on the new tokens of n_seqs sequences, packed one sequence after another: rows
+ * q_start[s] .. q_start[s+1] - 1 of q, k, v, out and lse belong to sequence s, and kv_len[s]
+ * counts the tokens that its cache holds once they are in it.  New token i (of n) of a sequence so
+ * has position p = kv_len[s] - n + i, and attends the tokens j <= p of its sequence:
+ *     t_j = scale * <q, k_j>    m = max t_j    l = sum exp(t_j - m)
+ *     out = sum exp(t_j - m) v_j / l           lse = m + ln l
+ * A row without any token to attend (p < 0) has out = 0 and lse = -infinity.  Query head h reads
+ * key/value head h / (heads / kv_heads).  Products are accumulated, and m, l and the sums held, in
+ * fp32; exp(t_j - m) is rounded to the cache's type for the second product, out once at the end.
+ */
+typedef struct vq_attn_desc {
+  int32_t heads;        /* query heads, at most 1024                                  */
+  int32_t kv_heads;     /* key/value heads; divides heads                             */
+  int32_t head_dim;     /* 64, 96, 128 or 256                                         */
+  int32_t page_size;    /* tokens in a page: 16, 32, 64 or 128                        */
+  int32_t n_pages;      /* pages in a K or V buffer                                   */
+  int32_t dtype;        /* VQ_F16 or VQ_BF16: q, k, v, the cache and out              */
+  float scale;          /* of the logits: positive and finite, as 1 / sqrt(head_dim)  */
+  int32_t reserved;     /* 0                                                          */
+} vq_attn_desc;
+
+/* The sequences of a call.  The three arrays are DEVICE memory and are read by the kernels, so a
+ * captured graph follows their contents.  Page numbers outside [0, n_pages) are read as a page
+ * inside (attention: that sequence's rows are then unspecified) and never written. */
+typedef struct vq_attn_batch {
+  int32_t n_seqs;             /* sequences, [1, 65536]                                               */
+  int32_t n_tokens;           /* new tokens of all sequences together (rows of q, k, v, out), >= 1   */
+  int32_t table_width;        /* pages that a row of page_table lists, >= 1                          */
+  int32_t max_len;            /* no kv_len is larger, [0, table_width * page_size]: decides how the
+                                 work is split; a larger kv_len is taken as max_len                  */
+  const int32_t* q_start;     /* [n_seqs + 1], ascending from 0 to n_tokens; NULL: one new token for
+                                 each sequence (n_tokens = n_seqs)                                   */
+  const int32_t* kv_len;      /* [n_seqs]                                                            */
+  const int32_t* page_table;  /* [n_seqs][table_width]; entries beyond a sequence's length are not read */
+} vq_attn_batch;
+
+/* Element strides of a [token][head][dim] array.  Two orders are read and written in whole vectors: dim = 1 with token
+ * and head multiples of 8, and token = 1 with dim and head multiples of 8 (a product Y[features, tokens] of
+ * vq_gemm_batched with row stride ldy is token = 1, head = head_dim * ldy, dim = ldy); others an element at a time.
+ * Where there is one token, or one head, its stride is not looked at.  A NULL vq_strides means
+ * [token][heads][head_dim] without gaps.  Inputs may repeat rows (stride 0); elements of an output are distinct. */
+typedef struct vq_strides { int64_t token, head, dim; } vq_strides;
+
+/* Bytes of the K buffer, and of the V buffer, of one layer's cache (host pointer). */
+VQ_API int vq_cache_bytes(const vq_attn_desc* desc, size_t* bytes);
+
+/*
+ * The new tokens' keys and values into their pages, copied bit for bit; k and v are
+ * [n_tokens][kv_heads][head_dim] with the strides given.  Tokens with a negative position, or in
+ * a page outside the cache, are left out.  k, v, k_pages and v_pages are 16-byte aligned and do not
+ * overlap.  desc->scale is not used.  One launch.
+ */
+VQ_API int vq_cache_append(const vq_attn_desc* desc, const vq_attn_batch* batch,
+                           const void* k, const vq_strides* k_strides,
+                           const void* v, const vq_strides* v_strides,
+                           void* k_pages, void* v_pages, void* stream);
+
+/*
+ * Copies whole pages in n_buffers buffers (K and V buffers of any number of layers, all of
+ * desc's page shape): page from_to[2i] to page from_to[2i + 1], in every buffer, as if one pair after
+ * another.  buffers and from_to are HOST arrays, read during the call.  This is what the fork of a
+ * sequence needs (its last page, if it is not full) and what compaction needs (pages into holes).
+ * n_buffers in [1, 65536], n_pairs in [1, 2^30]; page numbers in [0, n_pages).  Pairs that do not
+ * depend on one another share a launch.
+ */
+VQ_API int vq_cache_copy(const vq_attn_desc* desc, int n_buffers, void* const* buffers,
+                         int n_pairs, const int32_t* from_to, void* stream);
+
+/*
+ * Bytes of the workspace that vq_attn_decode and vq_attn_prompt need for a batch of these sizes
+ * (host fields of `batch` only; at least 16).  The workspace is device memory owned by the caller,
+ * 16-byte aligned, and all zero before its first use; every call leaves it fit for the next.  Calls
+ * that share a workspace must not overlap in time.
+ */
+VQ_API int vq_attn_workspace_bytes(const vq_attn_desc* desc, const vq_attn_batch* batch, size_t* bytes);
+
+/*
+ * out[token][head][dim] for one new token of every sequence (n_tokens = n_seqs; q_start is not
+ * read), whose key and value are in the cache already.  lse_f32 (may be NULL): fp32
+ * [n_tokens][heads].  q and out are 16-byte aligned and must not alias.  The same call gives the
+ * same bits every time.
+ */
+VQ_API int vq_attn_decode(const vq_attn_desc* desc, const vq_attn_batch* batch,
+                          const void* q, const vq_strides* q_strides,
+                          const void* k_pages, const void* v_pages,
+                          void* out, const vq_strides* out_strides, float* lse_f32,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same for any number of new tokens of every sequence: whole prompts, or the next pieces of
+ * prompts whose earlier tokens are in the cache. */
+VQ_API int vq_attn_prompt(const vq_attn_desc* desc, const vq_attn_batch* batch,
+                          const void* q, const vq_strides* q_strides,
+                          const void* k_pages, const void* v_pages,
+                          void* out, const vq_strides* out_strides, float* lse_f32,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -17,12 +17,15 @@ __all__ = [
     "vq_status_string", "vq_version", "vq_canonical_bytes", "vq_layout_bytes",
     "vq_pack_layout", "vq_gemv", "vq_gemv_multi", "GemvMultiArgs", "VQLoraDesc", "vq_lora_workspace_bytes", "vq_gemv_lora",
     "vq_gemv_lora_multi", "vq_gemv_lora_multi_static", "vq_gemm_batched", "vq_decode_dense", "vq_em_assign", "vq_em_update",
+    "VQ_BF16", "VQAttnDesc", "VQAttnBatch", "VQStrides", "make_attn_desc", "AttnBatch", "attn_workspace", "vq_cache_bytes",
+    "vq_cache_append", "vq_cache_copy", "vq_attn_workspace_bytes", "vq_attn_decode", "vq_attn_prompt",
 ]
 
 VQ_F16 = 1
 VQ_F32 = 2
 VQ_I8 = 3      # codebook_dtype: int8 lookup tables with one fp16 scale per group
 VQ_I8_BN = 4   # the same plus blockwise normalisation (16 levels per group, a 4-bit code per 32 weights)
+VQ_BF16 = 5    # attention over the paged cache only
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libvq.so")
@@ -43,6 +46,25 @@ class VQLoraDesc(ctypes.Structure):
     """Mirror of `vq_lora_desc` (include/vq.h)."""
     _fields_ = [("A_f16", ctypes.c_void_p), ("B_f16", ctypes.c_void_p),
                 ("rank", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class VQAttnDesc(ctypes.Structure):
+    """Mirror of `vq_attn_desc` (include/vq.h)."""
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class VQAttnBatch(ctypes.Structure):
+    """Mirror of `vq_attn_batch` (include/vq.h)."""
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("table_width", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p)]
+
+
+class VQStrides(ctypes.Structure):
+    """Mirror of `vq_strides` (include/vq.h)."""
+    _fields_ = [("token", ctypes.c_int64), ("head", ctypes.c_int64), ("dim", ctypes.c_int64)]
 
 
 _LORA_STRUCT = struct.Struct("=QQii")   # the fields of VQLoraDesc
@@ -101,6 +123,18 @@ def lib() -> ctypes.CDLL:
         L.vq_em_assign.argtypes = [dp, vp, vp, vp, vp, vp]
         L.vq_em_update.restype = i32
         L.vq_em_update.argtypes = [dp, vp, vp, vp, vp, vp]
+        ap, bp, st = ctypes.POINTER(VQAttnDesc), ctypes.POINTER(VQAttnBatch), ctypes.POINTER(VQStrides)
+        L.vq_cache_bytes.restype = i32
+        L.vq_cache_bytes.argtypes = [ap, sz]
+        L.vq_cache_append.restype = i32
+        L.vq_cache_append.argtypes = [ap, bp, vp, st, vp, st, vp, vp, vp]
+        L.vq_cache_copy.restype = i32
+        L.vq_cache_copy.argtypes = [ap, i32, ctypes.POINTER(vp), i32, ctypes.POINTER(ctypes.c_int32), vp]
+        L.vq_attn_workspace_bytes.restype = i32
+        L.vq_attn_workspace_bytes.argtypes = [ap, bp, sz]
+        for name in ("vq_attn_decode", "vq_attn_prompt"):
+            getattr(L, name).restype = i32
+            getattr(L, name).argtypes = [ap, bp, vp, st, vp, vp, vp, st, vp, vp, ctypes.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -273,3 +307,93 @@ def vq_em_assign(desc: VQDesc, W_f32, hdiag_f32, cb_f32, assign_u8, stream=None)
 def vq_em_update(desc: VQDesc, W_f32, hdiag_f32, assign_u8, cb_f32_out, stream=None) -> None:
     _check(lib().vq_em_update(ctypes.byref(desc), _ptr(W_f32), _ptr(hdiag_f32), _ptr(assign_u8),
                               _ptr(cb_f32_out), _stream(stream)), "vq_em_update")
+
+
+def make_attn_desc(heads: int, kv_heads: int, head_dim: int, page_size: int, n_pages: int, dtype: int = VQ_F16,
+                   scale: float | None = None) -> VQAttnDesc:
+    """scale: of the logits; None means 1 / sqrt(head_dim)."""
+    return VQAttnDesc(heads, kv_heads, head_dim, page_size, n_pages, dtype, head_dim ** -0.5 if scale is None else scale, 0)
+
+
+class AttnBatch:
+    """The sequences of a call (build once, call as long as the arrays and these sizes stay; what the arrays hold may change).
+    Keeps references to the tensors.  kv_len: int32 [n_seqs]; page_table: int32 [n_seqs, table_width]; q_start: int32
+    [n_seqs + 1], or None for one new token of every sequence; max_len: no kv_len is larger (None: what the table can list)."""
+
+    def __init__(self, kv_len, page_table, n_tokens: int | None = None, max_len: int | None = None, q_start=None, page_size: int | None = None):
+        import torch
+        for what, t, dim in (("kv_len", kv_len, 1), ("page_table", page_table, 2), ("q_start", q_start, 1)):
+            if t is not None and (t.dtype != torch.int32 or t.dim() != dim or not t.is_contiguous()):
+                raise ValueError(f"AttnBatch: {what} is a contiguous int32 tensor of {dim} dimension(s)")
+        n = kv_len.shape[0]
+        if page_table.shape[0] != n or (q_start is not None and q_start.shape[0] != n + 1):
+            raise ValueError("AttnBatch: arrays of different numbers of sequences")
+        if n_tokens is None:
+            if q_start is not None:
+                raise ValueError("AttnBatch: n_tokens is needed with q_start")
+            n_tokens = n
+        if max_len is None:
+            if page_size is None:
+                raise ValueError("AttnBatch: max_len, or page_size to take what the table can list")
+            max_len = page_table.shape[1] * page_size
+        self.struct = VQAttnBatch(n, n_tokens, page_table.shape[1], max_len, _ptr(q_start) or None, _ptr(kv_len), _ptr(page_table))
+        self._keep = (kv_len, page_table, q_start)
+
+
+def _rows(t, batch: AttnBatch, heads: int, desc: VQAttnDesc, what: str):
+    """The strides of a [n_tokens, heads, head_dim] tensor; None where it has no gaps."""
+    if t.dim() != 3 or t.shape[0] != batch.struct.n_tokens or t.shape[1] != heads or t.shape[2] != desc.head_dim or t.element_size() != 2:
+        raise ValueError(f"{what}: a 16-bit tensor [{batch.struct.n_tokens}, {heads}, {desc.head_dim}] is wanted, not {t.dtype} {tuple(t.shape)}")
+    return None if t.is_contiguous() else ctypes.byref(VQStrides(*t.stride()))
+
+
+def vq_cache_bytes(desc: VQAttnDesc) -> int:
+    a = ctypes.c_size_t(0)
+    _check(lib().vq_cache_bytes(ctypes.byref(desc), ctypes.byref(a)), "vq_cache_bytes")
+    return a.value
+
+
+def vq_cache_append(desc: VQAttnDesc, batch: AttnBatch, k, v, k_pages, v_pages, stream=None) -> None:
+    """k, v: [n_tokens, kv_heads, head_dim] views (strides as vq_strides allows) of the new tokens."""
+    _check(lib().vq_cache_append(desc, batch.struct, _ptr(k), _rows(k, batch, desc.kv_heads, desc, "k"), _ptr(v),
+                                 _rows(v, batch, desc.kv_heads, desc, "v"), _ptr(k_pages), _ptr(v_pages), _stream(stream)), "vq_cache_append")
+
+
+def vq_cache_copy(desc: VQAttnDesc, buffers, from_to, stream=None) -> None:
+    """buffers: K and V buffers; from_to: (page, page) pairs, copied one after another in every buffer."""
+    flat = [int(p) for pair in from_to for p in pair]
+    if len(flat) != 2 * len(from_to):
+        raise ValueError("vq_cache_copy: from_to is a list of pairs")
+    _check(lib().vq_cache_copy(desc, len(buffers), (ctypes.c_void_p * len(buffers))(*[_ptr(b) for b in buffers]), len(from_to),
+                               (ctypes.c_int32 * len(flat))(*flat), _stream(stream)), "vq_cache_copy")
+
+
+def vq_attn_workspace_bytes(desc: VQAttnDesc, batch: AttnBatch) -> int:
+    a = ctypes.c_size_t(0)
+    _check(lib().vq_attn_workspace_bytes(desc, batch.struct, ctypes.byref(a)), "vq_attn_workspace_bytes")
+    return a.value
+
+
+def attn_workspace(desc: VQAttnDesc, batch: AttnBatch, device="cuda:0"):
+    """A workspace for vq_attn_decode and vq_attn_prompt, ready for use."""
+    import torch
+    return torch.zeros(vq_attn_workspace_bytes(desc, batch), dtype=torch.uint8, device=device)
+
+
+def _attn(call, name, desc, batch, q, k_pages, v_pages, out, workspace, lse, stream):
+    if lse is not None and (lse.dim() != 2 or lse.shape[0] != q.shape[0] or lse.shape[1] != desc.heads or lse.element_size() != 4
+                            or not lse.is_contiguous()):
+        raise ValueError(f"{name}: lse is a contiguous float32 tensor [n_tokens, heads]")
+    _check(call(desc, batch.struct, _ptr(q), _rows(q, batch, desc.heads, desc, "q"), _ptr(k_pages), _ptr(v_pages), _ptr(out),
+                _rows(out, batch, desc.heads, desc, "out"), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                _stream(stream)), name)
+
+
+def vq_attn_decode(desc: VQAttnDesc, batch: AttnBatch, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:
+    """q, out: [n_seqs, heads, head_dim] views (strides as vq_strides allows); lse: float32 [n_seqs, heads] or None."""
+    _attn(lib().vq_attn_decode, "vq_attn_decode", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream)
+
+
+def vq_attn_prompt(desc: VQAttnDesc, batch: AttnBatch, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:
+    """q, out: [n_tokens, heads, head_dim] views (strides as vq_strides allows); lse: float32 [n_tokens, heads] or None."""
+    _attn(lib().vq_attn_prompt, "vq_attn_prompt", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream)

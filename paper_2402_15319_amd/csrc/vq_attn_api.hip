@@ -1,0 +1,238 @@
+// Entry points of attention over the paged cache (include/vq.h): argument checks and the plan of
+// every launch, on the host.
+#include <math.h>
+#include <string.h>
+
+#include "vq_attn.h"
+
+namespace vq {
+namespace {
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+
+int hip_status(hipError_t e) { return e == hipSuccess ? VQ_OK : VQ_ERR_HIP; }
+
+int check_attn_desc(const vq_attn_desc* d, bool scaled) {
+  if (!d) return VQ_ERR_NULL;
+  if (d->heads < 1 || d->kv_heads < 1 || d->head_dim < 1 || d->page_size < 1 || d->n_pages < 1 || d->reserved != 0) return VQ_ERR_BAD_DESC;
+  if (d->heads % d->kv_heads != 0) return VQ_ERR_BAD_DESC;
+  if (d->heads > 1024) return VQ_ERR_UNSUPPORTED;
+  if (d->head_dim != 64 && d->head_dim != 96 && d->head_dim != 128 && d->head_dim != 256) return VQ_ERR_UNSUPPORTED;
+  if (d->page_size != 16 && d->page_size != 32 && d->page_size != 64 && d->page_size != 128) return VQ_ERR_UNSUPPORTED;
+  if (d->dtype != VQ_F16 && d->dtype != VQ_BF16) return VQ_ERR_UNSUPPORTED;
+  if (scaled && !(d->scale > 0.f && d->scale <= 3.402823466e38f)) return VQ_ERR_BAD_ARG;   // a NaN fails both
+  return VQ_OK;
+}
+
+// What the host can see of a batch; the arrays' contents are checked by the kernels.
+int check_batch_sizes(const vq_attn_desc& d, const vq_attn_batch* b) {
+  if (!b) return VQ_ERR_NULL;
+  if (b->n_seqs < 1 || b->n_seqs > 65536 || b->n_tokens < 1 || b->table_width < 1 || b->max_len < 0) return VQ_ERR_BAD_ARG;
+  if ((int64_t)b->max_len > (int64_t)b->table_width * d.page_size) return VQ_ERR_BAD_ARG;
+  return VQ_OK;
+}
+
+int check_batch(const vq_attn_desc& d, const vq_attn_batch* b, bool one_each) {
+  const int st = check_batch_sizes(d, b);
+  if (st != VQ_OK) return st;
+  if ((one_each || !b->q_start) && b->n_tokens != b->n_seqs) return VQ_ERR_BAD_ARG;
+  if (!b->kv_len || !b->page_table) return VQ_ERR_NULL;
+  if (!aligned4(b->kv_len) || !aligned4(b->page_table) || !aligned4(b->q_start)) return VQ_ERR_ALIGN;
+  return VQ_OK;
+}
+
+CacheArgs cache_args(const vq_attn_desc& d, const vq_attn_batch& b, bool one_each) {
+  CacheArgs c = {};
+  c.q_start = one_each ? nullptr : b.q_start;
+  c.kv_len = b.kv_len;
+  c.table = b.page_table;
+  c.n_seqs = b.n_seqs;
+  c.n_tokens = b.n_tokens;
+  c.table_width = b.table_width;
+  c.max_len = b.max_len;
+  c.n_pages = d.n_pages;
+  c.page_shift = __builtin_ctz((unsigned)d.page_size);
+  c.kv_heads = d.kv_heads;
+  return c;
+}
+
+constexpr int64_t kMostStride = int64_t(1) << 56;   // elements that an index may step over: offsets in bytes stay within 64 bits
+
+// The strides of a [n_tokens][heads][head_dim] array as the kernels take them (see vq_strides).
+int check_strides(const vq_strides* in, int n_tokens, int heads, int head_dim, bool output, Strides* out) {
+  if (!in) {
+    *out = {(int64_t)heads * head_dim, head_dim, 1};
+    return VQ_OK;
+  }
+  Strides s = {n_tokens > 1 ? in->token : 0, heads > 1 ? in->head : 0, in->dim};
+  if (s.token < 0 || s.head < 0 || s.dim < 1) return VQ_ERR_BAD_ARG;
+  if (s.token > kMostStride / n_tokens || s.head > kMostStride / heads || s.dim > kMostStride / head_dim) return VQ_ERR_BAD_ARG;
+  if (output) {   // no two elements at one place: each stride spans what the smaller ones reach
+    struct { int64_t stride, extent; } e[3] = {{s.token, n_tokens}, {s.head, heads}, {s.dim, head_dim}};
+    for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < 2 - i; ++j)
+        if (e[j].stride > e[j + 1].stride) { const auto t = e[j]; e[j] = e[j + 1]; e[j + 1] = t; }
+    int64_t reach = 1;   // elements from the first to behind the last
+    for (int i = 0; i < 3; ++i) {
+      if (e[i].extent == 1) continue;
+      if (e[i].stride < reach) return VQ_ERR_BAD_ARG;
+      reach += e[i].stride * (e[i].extent - 1);
+    }
+  }
+  *out = s;
+  return VQ_OK;
+}
+
+int attn_workspace(const vq_attn_desc& d, const vq_attn_batch& b, size_t* bytes) {
+  (void)d;
+  (void)b;
+  *bytes = 16;
+  return VQ_OK;
+}
+
+int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,
+              const void* v_pages, void* out, const vq_strides* out_strides, float* lse_f32, void* workspace, size_t workspace_bytes,
+              void* stream, bool decode) {
+  int st = check_attn_desc(desc, true);
+  if (st != VQ_OK) return st;
+  st = check_batch(*desc, batch, decode);
+  if (st != VQ_OK) return st;
+  if (!q || !k_pages || !v_pages || !out || !workspace) return VQ_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(workspace) || !aligned4(lse_f32)) return VQ_ERR_ALIGN;
+  if (q == out || k_pages == out || v_pages == out) return VQ_ERR_BAD_ARG;
+  AttnArgs a = {};
+  st = check_strides(q_strides, batch->n_tokens, desc->heads, desc->head_dim, false, &a.qs);
+  if (st != VQ_OK) return st;
+  st = check_strides(out_strides, batch->n_tokens, desc->heads, desc->head_dim, true, &a.os);
+  if (st != VQ_OK) return st;
+  size_t need = 0;
+  st = attn_workspace(*desc, *batch, &need);
+  if (st != VQ_OK) return st;
+  if (workspace_bytes < need) return VQ_ERR_BAD_ARG;
+  a.c = cache_args(*desc, *batch, decode);
+  a.q = (const uint16_t*)q;
+  a.k_pages = (const uint16_t*)k_pages;
+  a.v_pages = (const uint16_t*)v_pages;
+  a.out = (uint16_t*)out;
+  a.lse = lse_f32;
+  a.heads = desc->heads;
+  a.group = desc->heads / desc->kv_heads;
+  a.scale_log2 = desc->scale * 1.44269504088896f;
+  const bool bf16 = desc->dtype == VQ_BF16;
+  return hip_status(decode ? launch_attn_decode(a, desc->head_dim, bf16, (hipStream_t)stream)
+                           : launch_attn_prompt(a, desc->head_dim, bf16, (hipStream_t)stream));
+}
+
+}  // namespace
+}  // namespace vq
+
+using namespace vq;
+
+extern "C" {
+
+int vq_cache_bytes(const vq_attn_desc* desc, size_t* bytes) {
+  const int st = check_attn_desc(desc, false);
+  if (st != VQ_OK) return st;
+  if (!bytes) return VQ_ERR_NULL;
+  *bytes = (size_t)desc->n_pages * desc->kv_heads * desc->page_size * desc->head_dim * 2;
+  return VQ_OK;
+}
+
+int vq_cache_append(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* k, const vq_strides* k_strides, const void* v,
+                    const vq_strides* v_strides, void* k_pages, void* v_pages, void* stream) {
+  int st = check_attn_desc(desc, false);
+  if (st != VQ_OK) return st;
+  st = check_batch(*desc, batch, false);
+  if (st != VQ_OK) return st;
+  if (!k || !v || !k_pages || !v_pages) return VQ_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages)) return VQ_ERR_ALIGN;
+  if (k_pages == v_pages || k == k_pages || k == v_pages || v == k_pages || v == v_pages) return VQ_ERR_BAD_ARG;
+  AppendArgs a = {};
+  st = check_strides(k_strides, batch->n_tokens, desc->kv_heads, desc->head_dim, false, &a.ks);
+  if (st != VQ_OK) return st;
+  st = check_strides(v_strides, batch->n_tokens, desc->kv_heads, desc->head_dim, false, &a.vs);
+  if (st != VQ_OK) return st;
+  a.c = cache_args(*desc, *batch, false);
+  a.k = (const uint16_t*)k;
+  a.v = (const uint16_t*)v;
+  a.k_pages = (uint16_t*)k_pages;
+  a.v_pages = (uint16_t*)v_pages;
+  return hip_status(launch_append(a, desc->head_dim, (hipStream_t)stream));
+}
+
+int vq_cache_copy(const vq_attn_desc* desc, int n_buffers, void* const* buffers, int n_pairs, const int32_t* from_to, void* stream) {
+  const int st = check_attn_desc(desc, false);
+  if (st != VQ_OK) return st;
+  if (n_buffers < 1 || n_buffers > 65536 || n_pairs < 1 || n_pairs > (1 << 30)) return VQ_ERR_BAD_ARG;
+  if (!buffers || !from_to) return VQ_ERR_NULL;
+  for (int i = 0; i < n_buffers; ++i) {
+    if (!buffers[i]) return VQ_ERR_NULL;
+    if (!aligned16(buffers[i])) return VQ_ERR_ALIGN;
+  }
+  for (size_t i = 0; i < 2 * (size_t)n_pairs; ++i)
+    if (from_to[i] < 0 || from_to[i] >= desc->n_pages) return VQ_ERR_BAD_ARG;
+  // Launches of one stream follow one another, so what depends on an earlier pair starts a new one.  The pages of a launch
+  // are held in a small hash table (open addressing, at most half full): 1 read, 2 written.
+  constexpr int kSlots = 2048;
+  static_assert(kSlots >= 4 * kCopyPairs, "half full at most");
+  CopyArgs a;
+  a.page_bytes = (uint64_t)desc->kv_heads * desc->page_size * desc->head_dim * 2;
+  for (int first = 0; first < n_pairs;) {
+    int32_t page[kSlots];
+    uint8_t use[kSlots];
+    memset(use, 0, sizeof(use));
+    const auto slot = [&](int32_t p) {
+      uint32_t h = ((uint32_t)p * 2654435761u) >> 21;
+      while (use[h] && page[h] != p) h = (h + 1) & (kSlots - 1);
+      return h;
+    };
+    int n = 0, i = first;
+    for (; i < n_pairs && n < kCopyPairs; ++i) {
+      const int32_t from = from_to[2 * (size_t)i], to = from_to[2 * (size_t)i + 1];
+      if (from == to) continue;
+      if (use[slot(to)] || use[slot(from)] == 2) break;
+      const uint32_t f = slot(from);
+      page[f] = from;
+      use[f] = 1;
+      const uint32_t t = slot(to);
+      page[t] = to;
+      use[t] = 2;
+      a.from_to[n][0] = from;
+      a.from_to[n][1] = to;
+      ++n;
+    }
+    first = i;
+    if (n == 0) continue;   // pages onto themselves only
+    a.n_pairs = n;
+    for (int b = 0; b < n_buffers; b += kCopyBuffers) {
+      a.n_buffers = n_buffers - b < kCopyBuffers ? n_buffers - b : kCopyBuffers;
+      memcpy(a.buffer, buffers + b, (size_t)a.n_buffers * sizeof(void*));
+      if (launch_copy(a, (hipStream_t)stream) != hipSuccess) return VQ_ERR_HIP;
+    }
+  }
+  return VQ_OK;
+}
+
+int vq_attn_workspace_bytes(const vq_attn_desc* desc, const vq_attn_batch* batch, size_t* bytes) {
+  int st = check_attn_desc(desc, false);
+  if (st != VQ_OK) return st;
+  st = check_batch_sizes(*desc, batch);
+  if (st != VQ_OK) return st;
+  if (!bytes) return VQ_ERR_NULL;
+  return attn_workspace(*desc, *batch, bytes);
+}
+
+int vq_attn_decode(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,
+                   const void* v_pages, void* out, const vq_strides* out_strides, float* lse_f32, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  return attn_impl(desc, batch, q, q_strides, k_pages, v_pages, out, out_strides, lse_f32, workspace, workspace_bytes, stream, true);
+}
+
+int vq_attn_prompt(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,
+                   const void* v_pages, void* out, const vq_strides* out_strides, float* lse_f32, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  return attn_impl(desc, batch, q, q_strides, k_pages, v_pages, out, out_strides, lse_f32, workspace, workspace_bytes, stream, false);
+}
+
+}  // extern "C"
