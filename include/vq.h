@@ -306,11 +306,11 @@ typedef struct vq_attn_desc {
  * captured graph follows their contents.  Page numbers outside [0, n_pages) are read as a page
  * inside (attention: that sequence's rows are then unspecified) and never written. */
 typedef struct vq_attn_batch {
-  int32_t n_seqs;             /* sequences, [1, 65536]                                               */
+  int32_t n_seqs;             /* sequences, [1, 65535]                                               */
   int32_t n_tokens;           /* new tokens of all sequences together (rows of q, k, v, out), >= 1   */
   int32_t table_width;        /* pages that a row of page_table lists, >= 1                          */
-  int32_t max_len;            /* no kv_len is larger, [0, table_width * page_size]: decides how the
-                                 work is split; a larger kv_len is taken as max_len                  */
+  int32_t max_len;            /* no kv_len is larger; [0, table_width * page_size], at most 2^29.
+                                 Decides how the work is split; a larger kv_len is taken as max_len  */
   const int32_t* q_start;     /* [n_seqs + 1], ascending from 0 to n_tokens; NULL: one new token for
                                  each sequence (n_tokens = n_seqs)                                   */
   const int32_t* kv_len;      /* [n_seqs]                                                            */

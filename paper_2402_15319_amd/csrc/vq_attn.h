@@ -42,6 +42,26 @@ struct AttnArgs {
   float scale_log2;    // scale * log2(e): the kernels work with powers of two
 };
 
+// How a call of vq_attn_decode is split: a workgroup takes `chunk` tokens of one sequence and up to 16 query heads of one
+// key/value head (a tile); where a sequence has several parts, the last of their workgroups to finish joins them.
+struct DecodePlan {
+  int32_t chunk, parts;   // tokens of a part; parts of the longest sequence
+  int32_t tiles, cols;    // tiles of a key/value head's query heads; query heads of a tile at most
+};
+constexpr int kJoinCounters = 16384;   // at the start of the workspace: parts that have finished, zero between calls
+constexpr int kTileHeads = 16;
+constexpr int kMostParts = 256;        // of a sequence
+
+struct DecodeArgs {
+  AttnArgs a;
+  DecodePlan plan;
+  uint32_t* counter;   // [n_seqs][kv_heads][tiles]
+  float* part;         // [n_seqs][kv_heads][tiles][parts][part_floats]
+};
+
+// What a part leaves: 16 maxima, 16 sums of weights, and sums over the values for each head of the tile.
+__host__ __device__ inline size_t part_floats(const DecodePlan& p, int head_dim) { return 2 * kTileHeads + (size_t)p.cols * head_dim; }
+
 // Pages copied by one launch: every pair in every buffer.  No page of a launch is written twice, or read and written.
 constexpr int kCopyBuffers = 128, kCopyPairs = 320;
 struct CopyArgs {
@@ -54,7 +74,7 @@ static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
 
 hipError_t launch_append(const AppendArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_copy(const CopyArgs& a, hipStream_t s);
-hipError_t launch_attn_decode(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_attn_decode(const DecodeArgs& a, int head_dim, bool bf16, hipStream_t s);
 hipError_t launch_attn_prompt(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s);
 
 }  // namespace vq

@@ -25,10 +25,12 @@ int check_attn_desc(const vq_attn_desc* d, bool scaled) {
   return VQ_OK;
 }
 
+constexpr int kMostLen = 1 << 29;   // tokens of a sequence: the kernels' token indexes stay within 32 bits with room to spare
+
 // What the host can see of a batch; the arrays' contents are checked by the kernels.
 int check_batch_sizes(const vq_attn_desc& d, const vq_attn_batch* b) {
   if (!b) return VQ_ERR_NULL;
-  if (b->n_seqs < 1 || b->n_seqs > 65536 || b->n_tokens < 1 || b->table_width < 1 || b->max_len < 0) return VQ_ERR_BAD_ARG;
+  if (b->n_seqs < 1 || b->n_seqs > 65535 || b->n_tokens < 1 || b->table_width < 1 || b->max_len < 0 || b->max_len > kMostLen) return VQ_ERR_BAD_ARG;
   if ((int64_t)b->max_len > (int64_t)b->table_width * d.page_size) return VQ_ERR_BAD_ARG;
   return VQ_OK;
 }
@@ -84,10 +86,39 @@ int check_strides(const vq_strides* in, int n_tokens, int heads, int head_dim, b
   return VQ_OK;
 }
 
+// Workgroups that keep the card busy, and the tokens that a part has at least and at most.
+constexpr int64_t kEnoughParts = 768;
+constexpr int kPartStep = 128, kPartMost = 4096;
+
+DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
+  DecodePlan p;
+  const int group = d.heads / d.kv_heads;
+  p.tiles = (group + kTileHeads - 1) / kTileHeads;
+  p.cols = group < kTileHeads ? group : kTileHeads;
+  const int64_t units = (int64_t)b.n_seqs * d.kv_heads * p.tiles;
+  const int64_t steps = ((int64_t)b.max_len + kPartStep - 1) / kPartStep;
+  int64_t parts = 1;
+  if (units <= kJoinCounters && steps > 1) {
+    parts = (kEnoughParts + units - 1) / units;
+    const int64_t least = (steps * kPartStep + kPartMost - 1) / kPartMost;
+    parts = parts < least ? least : parts;
+    parts = parts < kMostParts ? parts : kMostParts;
+    parts = parts < steps ? parts : steps;
+    const int64_t per = (steps + parts - 1) / parts;   // steps of a part
+    parts = (steps + per - 1) / per;
+    p.chunk = (int32_t)(per * kPartStep);
+  } else {
+    p.chunk = (int32_t)(steps < 1 ? kPartStep : steps * kPartStep);
+  }
+  p.parts = (int32_t)parts;
+  return p;
+}
+
 int attn_workspace(const vq_attn_desc& d, const vq_attn_batch& b, size_t* bytes) {
-  (void)d;
-  (void)b;
+  const DecodePlan p = decode_plan(d, b);
   *bytes = 16;
+  if (b.n_tokens == b.n_seqs && p.parts > 1)
+    *bytes = kJoinCounters * sizeof(uint32_t) + (size_t)b.n_seqs * d.kv_heads * p.tiles * p.parts * part_floats(p, d.head_dim) * sizeof(float);
   return VQ_OK;
 }
 
@@ -101,7 +132,8 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   if (!q || !k_pages || !v_pages || !out || !workspace) return VQ_ERR_NULL;
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(workspace) || !aligned4(lse_f32)) return VQ_ERR_ALIGN;
   if (q == out || k_pages == out || v_pages == out) return VQ_ERR_BAD_ARG;
-  AttnArgs a = {};
+  DecodeArgs both = {};
+  AttnArgs& a = both.a;
   st = check_strides(q_strides, batch->n_tokens, desc->heads, desc->head_dim, false, &a.qs);
   if (st != VQ_OK) return st;
   st = check_strides(out_strides, batch->n_tokens, desc->heads, desc->head_dim, true, &a.os);
@@ -120,8 +152,11 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   a.group = desc->heads / desc->kv_heads;
   a.scale_log2 = desc->scale * 1.44269504088896f;
   const bool bf16 = desc->dtype == VQ_BF16;
-  return hip_status(decode ? launch_attn_decode(a, desc->head_dim, bf16, (hipStream_t)stream)
-                           : launch_attn_prompt(a, desc->head_dim, bf16, (hipStream_t)stream));
+  if (!decode) return hip_status(launch_attn_prompt(a, desc->head_dim, bf16, (hipStream_t)stream));
+  both.plan = decode_plan(*desc, *batch);
+  both.counter = (uint32_t*)workspace;
+  both.part = (float*)workspace + kJoinCounters;
+  return hip_status(launch_attn_decode(both, desc->head_dim, bf16, (hipStream_t)stream));
 }
 
 }  // namespace

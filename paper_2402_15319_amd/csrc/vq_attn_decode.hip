@@ -1,72 +1,281 @@
-// Attention over the paged cache, plainly: one wave per (new token, query head).
+// Attention of one new token of every sequence over the paged cache.
 #include "vq_attn_device.h"
 
 namespace vq {
 namespace {
 
-// 64 tokens at a time, one a lane, for the logits; then the lanes take dimensions and go through the 64 tokens' values.
-// The running maximum and sum are those of a softmax in one pass: both, and the sums over the values, are scaled down
-// whenever the maximum grows.
-template <bool BF16>
-__global__ __launch_bounds__(64) void attn_plain_kernel(const AttnArgs a, int head_dim) {
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-  const int s = sequence_of(a.c, t);
-  int first, last;
-  rows_of(a.c, s, &first, &last);
-  if (t < first || t >= last) return;
-  const int n = cached_tokens(a.c, s) - last + t + 1;   // tokens that this row attends
-  const int size = 1 << a.c.page_shift;
-  const uint16_t* q = a.q + t * a.qs.token + h * a.qs.head;
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int j0 = 0; j0 < n; j0 += 64) {
-    const int j = j0 + lane;
-    const int page = page_inside(a.c, s, (j < n ? j : n - 1) >> a.c.page_shift);
-    const int64_t base = ((int64_t)page * a.c.kv_heads + h / a.group) * size * head_dim;
-    float x = -INFINITY;
-    if (j < n) {
-      const uint16_t* k = a.k_pages + base + (j & (size - 1)) * head_dim;
-      x = 0.f;
-      for (int d = 0; d < head_dim; ++d) x = fmaf(to_f32<BF16>(q[d * a.qs.dim]), to_f32<BF16>(k[d]), x);
-      x *= a.scale_log2;
+constexpr int kWaves = 4;
+
+// One workgroup: `chunk` tokens of a sequence, the query heads (up to 16) of a tile.  Its waves take 32 tokens at a time in turn.
+//   S^T = K Q^T: two instructions' rows are 16 tokens each, their columns the query heads.  The rows' tokens are chosen so that lane
+//   L ends up with the logits of tokens 8 (L / 16) .. + 7 of head L % 16, which is just the operand that
+//   O^T += V^T P^T takes: neither product moves anything between lanes, and a page's V is laid out so that V^T is read as it lies.
+// m and the sums are those of a softmax in one pass; a lane adds up its own weights until the end.
+template <bool BF16, int D>
+__global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A) {
+  constexpr int KS = D / 32, DT = D / 16;
+  const AttnArgs& a = A.a;
+  const int part = blockIdx.x, s = blockIdx.z;
+  const int kvh = blockIdx.y / A.plan.tiles, tile = blockIdx.y - kvh * A.plan.tiles;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int len = cached_tokens(a.c, s);
+  const int begin = part * A.plan.chunk;
+  if (begin >= len && part > 0) return;
+  const int end = len - begin < A.plan.chunk ? len : begin + A.plan.chunk;
+  const int h0 = kvh * a.group + tile * kTileHeads;                 // first query head
+  const int cols = a.group - tile * kTileHeads < kTileHeads ? a.group - tile * kTileHeads : kTileHeads;
+  const int shift = a.c.page_shift, mask = (1 << shift) - 1;
+
+  u32x4 q[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) q[k] = {0, 0, 0, 0};
+  if (col < cols) {
+    const uint16_t* row = a.q + s * a.qs.token + (h0 + col) * a.qs.head;
+    if (a.qs.dim == 1 && ((a.qs.token | a.qs.head) & 7) == 0) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) q[k] = *reinterpret_cast<const u32x4*>(row + 32 * k + 8 * g);
+    } else {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int64_t d = 32 * k + 8 * g + 2 * i;
+          q[k][i] = row[d * a.qs.dim] | (uint32_t)row[(d + 1) * a.qs.dim] << 16;
+        }
     }
-    float top = x;
-    for (int b = 1; b < 64; b <<= 1) top = fmaxf(top, __shfl_xor(top, b));
-    const float m_new = fmaxf(m, top);
-    const float zero = m_new == -INFINITY ? 0.f : m_new;
-    const float p = exp2f(x - zero), shrink = exp2f(m - zero);
-    float sum = p;
-    for (int b = 1; b < 64; b <<= 1) sum += __shfl_xor(sum, b);
-    l = l * shrink + sum;
+  }
+
+  const int64_t head_page = (int64_t)D << shift;                    // values of a head in a page
+  const int last_page = len > 0 ? (len - 1) >> shift : 0;
+  // Where the lane's rows of K (8 tokens of a page: row L % 16 is token 8 (L % 16 / 4) + L % 4, and 4 more in the second
+  // instruction) and its 8 tokens of V^T start, for the 32 tokens at t0.
+  const int k_run = (col >> 2) * 8, k_in = col & 3;
+  u32x4 kf[2][KS], vf[DT];
+  auto load_k = [&](int t0) {
+    const int t = t0 + k_run;
+    const int page = page_inside(a.c, s, t >> shift < last_page ? t >> shift : last_page);
+    const uint16_t* base = a.k_pages + ((int64_t)page * a.c.kv_heads + kvh) * head_page + ((t & mask) + k_in) * D + 8 * g;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      kf[0][k] = *reinterpret_cast<const u32x4*>(base + 32 * k);
+      kf[1][k] = *reinterpret_cast<const u32x4*>(base + 4 * D + 32 * k);
+    }
+  };
+  auto load_v = [&](int t0) {
+    const int t = t0 + 8 * g;
+    const int page = page_inside(a.c, s, t >> shift < last_page ? t >> shift : last_page);
+    const uint16_t* base = a.v_pages + ((int64_t)page * a.c.kv_heads + kvh) * head_page + ((int64_t)col << shift) + (t & mask);
+#pragma unroll
+    for (int i = 0; i < DT; ++i) vf[i] = *reinterpret_cast<const u32x4*>(base + ((int64_t)(16 * i) << shift));
+  };
+
+  float m = -INFINITY, l = 0.f;
+  f32x4 o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) o[i] = {0.f, 0.f, 0.f, 0.f};
+  int t0 = begin + 32 * wave;
+  if (t0 < end) {
+    load_k(t0);
+    load_v(t0);
+  }
+  for (; t0 < end; t0 += 32 * kWaves) {
+    const int next = t0 + 32 * kWaves;
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      s0 = mfma16<BF16>(kf[0][k], q[k], s0);
+      s1 = mfma16<BF16>(kf[1][k], q[k], s1);
+    }
+    if (next < end) load_k(next);
+    f32x8 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = s0[i] * a.scale_log2;
+      x[4 + i] = s1[i] * a.scale_log2;
+    }
+    if (t0 + 32 > len) {   // beyond the last token: no weight, and values that are not numbers must not meet it
+      const int rest = len - t0 - 8 * g;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = i < rest ? x[i] : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vf[i][j] = 2 * j + 1 < rest ? vf[i][j] : 2 * j < rest ? vf[i][j] & 0xffffu : 0u;
+    }
+    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m_new = fmaxf(m, top - kLift<BF16>);
+    const float from = m_new == -INFINITY ? 0.f : m_new;   // nothing but -infinity so far
+    const float shrink = exp2_fast(m - from);
     m = m_new;
-    for (int i = 0; i < 4; ++i) o[i] *= shrink;
-    const int most = n - j0 < 64 ? n - j0 : 64;
-    for (int r = 0; r < most; ++r) {
-      const float pr = __shfl(p, r);
-      const int64_t from = __shfl(base, r) + ((j0 + r) & (size - 1));
-      for (int i = 0; i < 4; ++i) {
-        const int d = lane + 64 * i;
-        if (d < head_dim) o[i] = fmaf(pr, to_f32<BF16>(a.v_pages[from + (int64_t)d * size]), o[i]);
+    f32x8 p;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = exp2_fast(x[i] - from);
+      sum += p[i];
+    }
+    l = l * shrink + sum;
+    const u32x4 pf = pack8<BF16>(p);
+#pragma unroll
+    for (int i = 0; i < DT; ++i) {
+      o[i] *= shrink;
+      o[i] = mfma16<BF16>(vf[i], pf, o[i]);
+    }
+    if (next < end) load_v(next);
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+
+  // The waves' sums, brought to one maximum: four values of a head a thread.
+  constexpr int kThreads = 64 * kWaves;
+  __shared__ float wave_m[kWaves][kTileHeads], wave_l[kWaves][kTileHeads];
+  __shared__ __attribute__((aligned(16))) float wave_o[kWaves][kTileHeads * D];
+  __shared__ uint32_t arrived;
+  if (g == 0) {
+    wave_m[wave][col] = m;
+    wave_l[wave][col] = l;
+  }
+  if (col < cols) {
+#pragma unroll
+    for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(&wave_o[wave][col * D + 16 * i + 4 * g]) = o[i];
+  }
+  __syncthreads();
+  const int parts = (len + A.plan.chunk - 1) / A.plan.chunk, quads = cols * (D / 4);
+  const int64_t unit = ((int64_t)s * a.c.kv_heads + kvh) * A.plan.tiles + tile;
+  const size_t part_size = part_floats(A.plan, D);
+  float* all = A.part + (size_t)unit * A.plan.parts * part_size;   // [part]: 16 maxima, 16 sums of weights, cols x D sums over values
+  // out and lse of four values of head c; an empty row has no weights
+  auto finish = [&](int i, f32x4 sum, float top, float weight) {
+    const int c = i / (D / 4), d = 4 * (i % (D / 4));
+    uint16_t* to = a.out + s * a.os.token + (h0 + c) * a.os.head + d * a.os.dim;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j * a.os.dim] = from_f32<BF16>(len > 0 ? sum[j] / weight : 0.f);
+    if (a.lse && d == 0) a.lse[(int64_t)s * a.heads + h0 + c] = len > 0 ? (top + __log2f(weight)) * 0.693147180559945f : -INFINITY;
+  };
+  for (int i = tid; i < quads; i += kThreads) {
+    const int c = i / (D / 4);
+    float top = wave_m[0][c];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_m[w][c]);
+    const float from = top == -INFINITY ? 0.f : top;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float weight = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = exp2_fast(wave_m[w][c] - from);
+      sum += f * *reinterpret_cast<const f32x4*>(&wave_o[w][4 * i]);
+      weight += f * wave_l[w][c];
+    }
+    if (parts <= 1) {
+      finish(i, sum, top, weight);
+    } else {
+      float* mine = all + part * part_size;
+      *reinterpret_cast<f32x4*>(mine + 2 * kTileHeads + 4 * i) = sum;
+      if (i % (D / 4) == 0) {
+        mine[c] = top;
+        mine[kTileHeads + c] = weight;
       }
     }
   }
-  uint16_t* out = a.out + t * a.os.token + h * a.os.head;
-  for (int i = 0; i < 4; ++i) {
-    const int d = lane + 64 * i;
-    if (d < head_dim) out[d * a.os.dim] = from_f32<BF16>(n > 0 ? o[i] / l : 0.f);
+  if (parts <= 1) return;
+
+  // Several parts: whoever finishes last joins them, in the parts' order.
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) arrived = __hip_atomic_fetch_add(&A.counter[unit], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (arrived != (uint32_t)parts - 1) return;
+  __threadfence();
+  if (tid == 0) __hip_atomic_store(&A.counter[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // The parts' factors: thread (head tid % 16, every 16th part).
+  constexpr int kEach = kMostParts / (kThreads / kTileHeads);
+  static_assert(kMostParts * kTileHeads <= kWaves * kTileHeads * D, "the factors fit where the waves' sums were");
+  float* factor = wave_o[0];                                        // [part][16]
+  __shared__ float some[kThreads / kTileHeads][kTileHeads];
+  const int c0 = tid % kTileHeads, r0 = tid / kTileHeads;
+  float pm[kEach], pl[kEach];
+  float top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int p = r0 + j * (kThreads / kTileHeads);
+    const bool there = p < parts && c0 < cols;
+    pm[j] = there ? all[p * part_size + c0] : -INFINITY;
+    pl[j] = there ? all[p * part_size + kTileHeads + c0] : 0.f;
   }
-  if (a.lse && lane == 0) a.lse[(int64_t)t * a.heads + h] = n > 0 ? (m + log2f(l)) * 0.693147180559945f : -INFINITY;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) top = fmaxf(top, pm[j]);
+  some[r0][c0] = top;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kThreads / kTileHeads; ++r) top = fmaxf(top, some[r][c0]);
+  const float from = top == -INFINITY ? 0.f : top;
+  float weight = 0.f;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int p = r0 + j * (kThreads / kTileHeads);
+    const float f = exp2_fast(pm[j] - from);
+    weight += f * pl[j];
+    if (p < parts) factor[p * kTileHeads + c0] = f;
+  }
+  __syncthreads();
+  some[r0][c0] = weight;
+  if (r0 == 0) wave_m[0][c0] = top;
+  __syncthreads();
+  if (r0 == 0) {
+    weight = 0.f;
+#pragma unroll
+    for (int r = 0; r < kThreads / kTileHeads; ++r) weight += some[r][c0];
+    wave_l[0][c0] = weight;
+  }
+  __syncthreads();
+  // The sums: where there are fewer groups of four values than threads, several threads share one, each with every
+  // `share`th part.
+  const int share = quads < kThreads ? kThreads / quads : 1, mine = share > 1 ? tid / quads : 0;
+  f32x4* shared_sum = reinterpret_cast<f32x4*>(wave_o[0]);
+  for (int i0 = 0; i0 < quads; i0 += kThreads) {
+    const int i = share > 1 ? tid % quads : i0 + tid, c = i / (D / 4);
+    const bool busy = i < quads && mine < share;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (busy) {
+      const float* from_part = all + 2 * kTileHeads + 4 * i;
+      int p = mine;
+      for (; p + 7 * share < parts; p += 8 * share) {
+        f32x4 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const f32x4*>(from_part + (p + j * share) * part_size);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += factor[(p + j * share) * kTileHeads + c] * v[j];
+      }
+      for (; p < parts; p += share) sum += factor[p * kTileHeads + c] * *reinterpret_cast<const f32x4*>(from_part + p * part_size);
+    }
+    if (share > 1) {   // quads < kThreads: one turn of the loop
+      __syncthreads();
+      if (busy) shared_sum[tid] = sum;
+      __syncthreads();
+      if (mine != 0) return;
+      for (int r = 1; r < share; ++r) sum += shared_sum[r * quads + i];
+    }
+    if (busy) finish(i, sum, wave_m[0][c], wave_l[0][c]);
+  }
 }
 
-hipError_t launch_plain(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s) {
-  const dim3 grid(a.c.n_tokens, a.heads);
-  if (bf16) attn_plain_kernel<true><<<grid, 64, 0, s>>>(a, head_dim);
-  else attn_plain_kernel<false><<<grid, 64, 0, s>>>(a, head_dim);
-  return hipGetLastError();
+template <bool BF16>
+void launch_type(const DecodeArgs& a, int head_dim, hipStream_t s) {
+  const dim3 grid(a.plan.parts, a.a.c.kv_heads * a.plan.tiles, a.a.c.n_seqs);
+  if (head_dim == 64) decode_kernel<BF16, 64><<<grid, 64 * kWaves, 0, s>>>(a);
+  else if (head_dim == 96) decode_kernel<BF16, 96><<<grid, 64 * kWaves, 0, s>>>(a);
+  else if (head_dim == 128) decode_kernel<BF16, 128><<<grid, 64 * kWaves, 0, s>>>(a);
+  else decode_kernel<BF16, 256><<<grid, 64 * kWaves, 0, s>>>(a);
 }
 
 }  // namespace
 
-hipError_t launch_attn_decode(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s) { return launch_plain(a, head_dim, bf16, s); }
-hipError_t launch_attn_prompt(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s) { return launch_plain(a, head_dim, bf16, s); }
+hipError_t launch_attn_decode(const DecodeArgs& a, int head_dim, bool bf16, hipStream_t s) {
+  if (bf16) launch_type<true>(a, head_dim, s);
+  else launch_type<false>(a, head_dim, s);
+  return hipGetLastError();
+}
 
 }  // namespace vq

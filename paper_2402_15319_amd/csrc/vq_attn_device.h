@@ -46,4 +46,30 @@ __device__ __forceinline__ int page_inside(const CacheArgs& c, int s, int j) {
   return (int)(p < (uint32_t)c.n_pages ? p : (uint32_t)c.n_pages - 1);
 }
 
+// Eight values of the cache's type, the share of a lane in an operand of a matrix instruction.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+// 16 x 16 += 16 x 32 . 32 x 16.  Lane L holds row (a) or column (b) L % 16 at k = 8 (L / 16) .. + 7, and of the result
+// column L % 16 at rows 4 (L / 16) .. + 3.
+template <bool BF16> __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Eight weights rounded to the cache's type.
+template <bool BF16> __device__ __forceinline__ u32x4 pack8(f32x8 p) {
+  if constexpr (BF16) return __builtin_bit_cast(u32x4, __builtin_convertvector(p, bf16x8));
+  else return __builtin_bit_cast(u32x4, __builtin_convertvector(p, f16x8));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp
+
+// Weights are exp2(x - m) with m the running maximum less this much: in fp16 a weight of 2^-14 and less would lose bits, so
+// the largest is 2^kLift there.  It cancels in out and in lse.
+template <bool BF16> constexpr float kLift = BF16 ? 0.f : 8.f;
+
 }  // namespace vq

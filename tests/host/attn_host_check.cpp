@@ -51,9 +51,22 @@ void check_attn(const AttnArgs& a, int head_dim) {
   REQUIRE(a.q && a.k_pages && a.v_pages && a.out && a.scale_log2 > 0 && a.group >= 1 && a.heads == a.group * a.c.kv_heads);
 }
 
-hipError_t launch_attn_decode(const AttnArgs& a, int head_dim, bool, hipStream_t) {
+hipError_t launch_attn_decode(const DecodeArgs& d, int head_dim, bool, hipStream_t) {
+  const AttnArgs& a = d.a;
+  const DecodePlan& p = d.plan;
   check_attn(a, head_dim);
   REQUIRE(!a.c.q_start && a.c.n_seqs == a.c.n_tokens);
+  // every token in a part, every query head in a tile, no part that the longest sequence leaves empty
+  REQUIRE(p.chunk >= 128 && p.chunk % 128 == 0 && p.parts >= 1 && p.parts <= kMostParts && (long long)p.chunk * p.parts >= a.c.max_len);
+  REQUIRE(p.parts == 1 || (long long)p.chunk * (p.parts - 1) < a.c.max_len);
+  REQUIRE((long long)p.chunk + a.c.max_len < 2147483647 - 1024);
+  REQUIRE(p.cols >= 1 && p.cols <= kTileHeads && p.tiles * kTileHeads >= a.group && p.cols == (a.group < kTileHeads ? a.group : kTileHeads));
+  if (p.parts > 1) {   // the workspace holds the counters and every part
+    const long long units = (long long)a.c.n_seqs * a.c.kv_heads * p.tiles;
+    REQUIRE(units <= kJoinCounters);
+    const size_t end = (size_t)((char*)d.part - (char*)d.counter) + (size_t)units * p.parts * part_floats(p, head_dim) * 4;
+    REQUIRE((char*)d.part - (char*)d.counter >= kJoinCounters * 4 && end <= g_workspace);
+  }
   return hipSuccess;
 }
 
@@ -108,10 +121,10 @@ static void calls(std::mt19937& rng) {
     d.dtype = rng() % 2 ? VQ_F16 : VQ_BF16;
     d.scale = 0.1f;
     vq_attn_batch b = {};
-    b.n_seqs = log_int(65536);
+    b.n_seqs = log_int(65535);
     const bool one_each = rng() % 2;
     b.n_tokens = one_each ? b.n_seqs : log_int(1 << 24);
-    b.table_width = log_int(2147483647 / d.page_size);
+    b.table_width = log_int((1 << 29) / d.page_size);
     b.max_len = rng() % 4 ? log_int(b.table_width * d.page_size) : b.table_width * d.page_size;
     b.kv_len = (const int32_t*)at(1);
     b.page_table = (const int32_t*)at(2);
@@ -133,6 +146,7 @@ static void calls(std::mt19937& rng) {
 }
 
 static void strides() {
+  vq::g_workspace = 1 << 30;
   vq_attn_desc d = {8, 2, 128, 16, 100, VQ_F16, 0.1f, 0};
   vq_attn_batch b = {4, 4, 10, 160, nullptr, (const int32_t*)at(1), (const int32_t*)at(2)};
   struct { vq_strides s; bool output; } good[] = {

@@ -56,7 +56,8 @@ def test_bad_scales(scale):
         assert _attn(name, _desc(scale=scale), _batch()) == ARG
 
 
-@pytest.mark.parametrize("change", [dict(n_seqs=0), dict(n_seqs=65537), dict(n_tokens=0), dict(table_width=0), dict(max_len=-1), dict(max_len=161)])
+@pytest.mark.parametrize("change", [dict(n_seqs=0), dict(n_seqs=65536), dict(n_tokens=0), dict(table_width=0), dict(max_len=-1), dict(max_len=161),
+                                    dict(max_len=2 ** 29 + 1, table_width=2 ** 27)])
 def test_bad_batches(change):
     assert _all(_desc(), _batch(**change)) == [ARG] * 4
 
