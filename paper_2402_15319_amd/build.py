@@ -22,6 +22,9 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
+# sources with flags of their own: attention keeps its accumulators in vector registers, where it scales them
+ACC_IN_VGPRS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+SOURCE_FLAGS = {"vq_attn_decode.hip": ACC_IN_VGPRS, "vq_attn_prompt.hip": ACC_IN_VGPRS}
 
 
 def _run(cmd, verbose):
@@ -42,7 +45,7 @@ def _link(sources, out, verbose):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
     objs = [os.path.join(OBJ_DIR, os.path.splitext(s)[0] + ".o") for s in sources]
-    cmds = [[hipcc, *HIPCC_FLAGS, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(sources, objs)]
+    cmds = [[hipcc, *HIPCC_FLAGS, *SOURCE_FLAGS.get(s, []), "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(sources, objs)]
     with ThreadPoolExecutor(max_workers=min(8, len(cmds))) as pool:
         list(pool.map(lambda c: _run(c, verbose), cmds))
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", out, *objs], verbose)

@@ -47,10 +47,11 @@ struct AttnArgs {
 struct DecodePlan {
   int32_t chunk, parts;   // tokens of a part; parts of the longest sequence
   int32_t tiles, cols;    // tiles of a key/value head's query heads; query heads of a tile at most
+  int32_t waves;          // of a workgroup: 4 or 8; each takes 32 tokens in turn
 };
 constexpr int kJoinCounters = 16384;   // at the start of the workspace: parts that have finished, zero between calls
 constexpr int kTileHeads = 16;
-constexpr int kMostParts = 256;        // of a sequence
+constexpr int kMostParts = 64;         // of a sequence
 
 struct DecodeArgs {
   AttnArgs a;

@@ -86,9 +86,10 @@ int check_strides(const vq_strides* in, int n_tokens, int heads, int head_dim, b
   return VQ_OK;
 }
 
-// Workgroups that keep the card busy, and the tokens that a part has at least and at most.
-constexpr int64_t kEnoughParts = 768;
-constexpr int kPartStep = 128, kPartMost = 4096;
+constexpr int kPartStep = 128;            // tokens that a workgroup takes at a time
+constexpr int64_t kEnoughUnits = 256;     // workgroups: one for each CU
+constexpr int kLongPart = 4096, kShortPart = 1024;
+constexpr int kShortValues = 32768;       // of a sequence's keys: no parts up to here
 
 DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   DecodePlan p;
@@ -96,21 +97,26 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   p.tiles = (group + kTileHeads - 1) / kTileHeads;
   p.cols = group < kTileHeads ? group : kTileHeads;
   const int64_t units = (int64_t)b.n_seqs * d.kv_heads * p.tiles;
-  const int64_t steps = ((int64_t)b.max_len + kPartStep - 1) / kPartStep;
+  const int64_t steps = b.max_len > kPartStep ? ((int64_t)b.max_len + kPartStep - 1) / kPartStep : 1;
   int64_t parts = 1;
-  if (units <= kJoinCounters && steps > 1) {
-    parts = (kEnoughParts + units - 1) / units;
-    const int64_t least = (steps * kPartStep + kPartMost - 1) / kPartMost;
-    parts = parts < least ? least : parts;
+  p.waves = 4;
+  if ((int64_t)b.max_len * d.head_dim <= kShortValues) {
+    // One part of 8 waves: a step or two for each of them cost less than the join (a sequence of 256 tokens x 32 heads of 128 6.1
+    // us, in two parts of 4 waves 7.7; of 512 8.9 and 8.0; of 512 x 32 heads of 64 5.6 and 7.7).
+    p.waves = b.max_len > 32 * p.waves ? 8 : 4;
+  } else if (units <= kJoinCounters) {
+    // A workgroup for every CU is enough where they are of one size (130,001 tokens x 8 heads: 256 workgroups 97 us, 512 100,
+    // 1,024 106).  Where there are as many without a split, the lengths will differ, and parts of 1,024 tokens even them
+    // out (61 sequences of 1 to 8,192: parts of 1,024 68 us, of 2,048 77, of 4,096 85; 24 of 2,048 to 4,096 alike: 203 and 202).
+    const int64_t most = units < kEnoughUnits ? kLongPart : kShortPart;
+    const int64_t enough = (kEnoughUnits + units - 1) / units, least = (steps * kPartStep + most - 1) / most;
+    parts = enough > least ? enough : least;
     parts = parts < kMostParts ? parts : kMostParts;
     parts = parts < steps ? parts : steps;
-    const int64_t per = (steps + parts - 1) / parts;   // steps of a part
-    parts = (steps + per - 1) / per;
-    p.chunk = (int32_t)(per * kPartStep);
-  } else {
-    p.chunk = (int32_t)(steps < 1 ? kPartStep : steps * kPartStep);
   }
-  p.parts = (int32_t)parts;
+  const int64_t per = (steps + parts - 1) / parts;   // steps of a part
+  p.parts = (int32_t)((steps + per - 1) / per);
+  p.chunk = (int32_t)(per * kPartStep);
   return p;
 }
 

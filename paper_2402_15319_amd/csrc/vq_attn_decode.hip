@@ -4,20 +4,22 @@
 namespace vq {
 namespace {
 
-constexpr int kWaves = 4;
-
 // One workgroup: `chunk` tokens of a sequence, the query heads (up to 16) of a tile.  Its waves take 32 tokens at a time in turn.
 //   S^T = K Q^T: two instructions' rows are 16 tokens each, their columns the query heads.  The rows' tokens are chosen so that lane
 //   L ends up with the logits of tokens 8 (L / 16) .. + 7 of head L % 16, which is just the operand that
 //   O^T += V^T P^T takes: neither product moves anything between lanes, and a page's V is laid out so that V^T is read as it lies.
 // m and the sums are those of a softmax in one pass; a lane adds up its own weights until the end.
-template <bool BF16, int D>
-__global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A) {
+// WHOLE_LINES: pages of at most 32 tokens, whose V a load reads in whole lines of memory that nobody reads again: they pass the
+// caches by (24 sequences of 2,000 to 4,096 tokens x 32 heads, pages of 16: 195 us, 217 without).  In larger pages a step's 64 bytes of a row of
+// V^T are half a line, and the wave with the other half wants it kept (130,001 tokens, pages of 64: 95 us, 107 if not); the
+// same holds for K, whose rows four instructions read in turn.
+template <bool BF16, int D, bool WHOLE_LINES, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void decode_kernel(const DecodeArgs A) {
   constexpr int KS = D / 32, DT = D / 16;
   const AttnArgs& a = A.a;
-  const int part = blockIdx.x, s = blockIdx.z;
-  const int kvh = blockIdx.y / A.plan.tiles, tile = blockIdx.y - kvh * A.plan.tiles;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int part = blockIdx.z, s = blockIdx.y;
+  const int kvh = blockIdx.x / A.plan.tiles, tile = blockIdx.x - kvh * A.plan.tiles;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int len = cached_tokens(a.c, s);
   const int begin = part * A.plan.chunk;
   if (begin >= len && part > 0) return;
@@ -51,79 +53,98 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A)
   // instruction) and its 8 tokens of V^T start, for the 32 tokens at t0.
   const int k_run = (col >> 2) * 8, k_in = col & 3;
   u32x4 kf[2][KS], vf[DT];
-  auto load_k = [&](int t0) {
-    const int t = t0 + k_run;
-    const int page = page_inside(a.c, s, t >> shift < last_page ? t >> shift : last_page);
-    const uint16_t* base = a.k_pages + ((int64_t)page * a.c.kv_heads + kvh) * head_page + ((t & mask) + k_in) * D + 8 * g;
+  const int32_t* table = a.c.table + (int64_t)s * a.c.table_width;
+  auto page_at = [&](int t) { return table[t >> shift < last_page ? t >> shift : last_page]; };
+  // (Behind the last step there is nothing to load: all lanes then read the buffer's first 16 bytes, so that the loop is one
+  // stretch of code in which every wait knows what is under way.)
+  auto load_k = [&](int t0, int page, bool there) {
+    const uint16_t* base = a.k_pages + ((int64_t)page_inside(a.c, page) * a.c.kv_heads + kvh) * head_page + (((t0 + k_run) & mask) + k_in) * D + 8 * g;
+    base = there ? base : a.k_pages;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       kf[0][k] = *reinterpret_cast<const u32x4*>(base + 32 * k);
       kf[1][k] = *reinterpret_cast<const u32x4*>(base + 4 * D + 32 * k);
     }
   };
-  auto load_v = [&](int t0) {
-    const int t = t0 + 8 * g;
-    const int page = page_inside(a.c, s, t >> shift < last_page ? t >> shift : last_page);
-    const uint16_t* base = a.v_pages + ((int64_t)page * a.c.kv_heads + kvh) * head_page + ((int64_t)col << shift) + (t & mask);
+  auto load_v = [&](int t0, int page, bool there) {
+    const uint16_t* base = a.v_pages + ((int64_t)page_inside(a.c, page) * a.c.kv_heads + kvh) * head_page + ((int64_t)col << shift) + ((t0 + 8 * g) & mask);
+    base = there ? base : a.v_pages;
 #pragma unroll
-    for (int i = 0; i < DT; ++i) vf[i] = *reinterpret_cast<const u32x4*>(base + ((int64_t)(16 * i) << shift));
+    for (int i = 0; i < DT; ++i) {
+      const u32x4* from = reinterpret_cast<const u32x4*>(base + ((int64_t)(16 * i) << shift));
+      if constexpr (WHOLE_LINES) vf[i] = __builtin_nontemporal_load(from);
+      else vf[i] = *from;
+    }
   };
 
-  float m = -INFINITY, l = 0.f;
+  // m: what the weights' exponents are taken from, the same in the four lanes of a head.  It follows the running maximum only
+  // where a logit is more than kSlack above it (weights are then up to 2^(kLift + kSlack)): most steps scale nothing.
+  float m = -INFINITY, from = 0.f, l = 0.f;   // from: m, or 0 while m is -infinity
   f32x4 o[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kStride = 32 * kWaves;
+  int k_page = 0, v_page = 0;   // of the step after the one whose loads are under way: no load waits for the table
   int t0 = begin + 32 * wave;
   if (t0 < end) {
-    load_k(t0);
-    load_v(t0);
+    k_page = page_at(t0 + k_run);
+    v_page = page_at(t0 + 8 * g);
+    load_k(t0, k_page, true);
+    load_v(t0, v_page, true);
+    k_page = page_at(t0 + kStride + k_run);
+    v_page = page_at(t0 + kStride + 8 * g);
   }
-  for (; t0 < end; t0 += 32 * kWaves) {
-    const int next = t0 + 32 * kWaves;
+  for (; t0 < end; t0 += kStride) {
+    const bool more = t0 + kStride < end;
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       s0 = mfma16<BF16>(kf[0][k], q[k], s0);
       s1 = mfma16<BF16>(kf[1][k], q[k], s1);
     }
-    if (next < end) load_k(next);
+    __builtin_amdgcn_sched_barrier(0);   // into the registers that the products have just read, not into others before them
+    load_k(t0 + kStride, k_page, more);
+    k_page = page_at(t0 + 2 * kStride + k_run);
     f32x8 x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       x[i] = s0[i] * a.scale_log2;
       x[4 + i] = s1[i] * a.scale_log2;
     }
-    if (t0 + 32 > len) {   // beyond the last token: no weight, and values that are not numbers must not meet it
+    if (t0 + 32 > len) {   // beyond the last token: no weight, and what is no number must not meet it
       const int rest = len - t0 - 8 * g;
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = i < rest ? x[i] : -INFINITY;
+      u32x4 keep;
 #pragma unroll
-      for (int i = 0; i < DT; ++i)
+      for (int j = 0; j < 4; ++j) keep[j] = (2 * j < rest ? 0xffffu : 0u) | (2 * j + 1 < rest ? 0xffff0000u : 0u);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) vf[i][j] = 2 * j + 1 < rest ? vf[i][j] : 2 * j < rest ? vf[i][j] & 0xffffu : 0u;
+      for (int i = 0; i < DT; ++i) vf[i] &= keep;
     }
     float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float m_new = fmaxf(m, top - kLift<BF16>);
-    const float from = m_new == -INFINITY ? 0.f : m_new;   // nothing but -infinity so far
-    const float shrink = exp2_fast(m - from);
-    m = m_new;
+    if (__any(top > m + (kLift<BF16> + kSlack))) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float old = m;
+      m = fmaxf(m, top - kLift<BF16>);
+      from = m == -INFINITY ? 0.f : m;
+      const float shrink = exp2_fast(old - from);
+      l *= shrink;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= shrink;
+    }
     f32x8 p;
-    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       p[i] = exp2_fast(x[i] - from);
-      sum += p[i];
+      l += p[i];
     }
-    l = l * shrink + sum;
     const u32x4 pf = pack8<BF16>(p);
 #pragma unroll
-    for (int i = 0; i < DT; ++i) {
-      o[i] *= shrink;
-      o[i] = mfma16<BF16>(vf[i], pf, o[i]);
-    }
-    if (next < end) load_v(next);
+    for (int i = 0; i < DT; ++i) o[i] = mfma16<BF16>(vf[i], pf, o[i]);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(t0 + kStride, v_page, more);
+    v_page = page_at(t0 + 2 * kStride + 8 * g);
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
@@ -145,7 +166,7 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A)
   const int parts = (len + A.plan.chunk - 1) / A.plan.chunk, quads = cols * (D / 4);
   const int64_t unit = ((int64_t)s * a.c.kv_heads + kvh) * A.plan.tiles + tile;
   const size_t part_size = part_floats(A.plan, D);
-  float* all = A.part + (size_t)unit * A.plan.parts * part_size;   // [part]: 16 maxima, 16 sums of weights, cols x D sums over values
+  float* all = A.part + (size_t)unit * A.plan.parts * part_size;   // [part]: 16 maxima and sums of weights, cols x D sums over values
   // out and lse of four values of head c; an empty row has no weights
   auto finish = [&](int i, f32x4 sum, float top, float weight) {
     const int c = i / (D / 4), d = 4 * (i % (D / 4));
@@ -172,25 +193,50 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A)
       finish(i, sum, top, weight);
     } else {
       float* mine = all + part * part_size;
-      *reinterpret_cast<f32x4*>(mine + 2 * kTileHeads + 4 * i) = sum;
-      if (i % (D / 4) == 0) {
-        mine[c] = top;
-        mine[kTileHeads + c] = weight;
-      }
+      shared_store(mine + 2 * kTileHeads + 4 * i, sum[0], sum[1]);
+      shared_store(mine + 2 * kTileHeads + 4 * i + 2, sum[2], sum[3]);
+      if (i % (D / 4) == 0) shared_store(mine + 2 * c, top, weight);
     }
   }
   if (parts <= 1) return;
 
   // Several parts: whoever finishes last joins them, in the parts' order.
-  __threadfence();
+  shared_stores_done();
   __syncthreads();
-  if (tid == 0) arrived = __hip_atomic_fetch_add(&A.counter[unit], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  if (tid == 0) arrived = __hip_atomic_fetch_add(&A.counter[unit], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (arrived != (uint32_t)parts - 1) return;
-  __threadfence();
   if (tid == 0) __hip_atomic_store(&A.counter[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  constexpr int kFew = 8;
+  if (parts <= kFew) {   // few: a thread asks for all it needs at once
+    for (int i = tid; i < quads; i += kThreads) {
+      f32x2 ml[kFew], v[kFew][2];
+#pragma unroll
+      for (int p = 0; p < kFew; ++p) {
+        const float* from = all + (p < parts ? p : 0) * part_size;
+        ml[p] = shared_load(from + 2 * (i / (D / 4)));
+        v[p][0] = shared_load(from + 2 * kTileHeads + 4 * i);
+        v[p][1] = shared_load(from + 2 * kTileHeads + 4 * i + 2);
+      }
+      float top = ml[0][0];
+#pragma unroll
+      for (int p = 1; p < kFew; ++p) top = fmaxf(top, ml[p][0]);
+      const float base = top == -INFINITY ? 0.f : top;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      float weight = 0.f;
+#pragma unroll
+      for (int p = 0; p < kFew; ++p) {
+        if (p >= parts) break;
+        const float f = exp2_fast(ml[p][0] - base);
+        sum += f * f32x4{v[p][0][0], v[p][0][1], v[p][1][0], v[p][1][1]};
+        weight += f * ml[p][1];
+      }
+      finish(i, sum, top, weight);
+    }
+    return;
+  }
   // The parts' factors: thread (head tid % 16, every 16th part).
-  constexpr int kEach = kMostParts / (kThreads / kTileHeads);
+  constexpr int kEach = (kMostParts + kThreads / kTileHeads - 1) / (kThreads / kTileHeads);
   static_assert(kMostParts * kTileHeads <= kWaves * kTileHeads * D, "the factors fit where the waves' sums were");
   float* factor = wave_o[0];                                        // [part][16]
   __shared__ float some[kThreads / kTileHeads][kTileHeads];
@@ -201,8 +247,9 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A)
   for (int j = 0; j < kEach; ++j) {
     const int p = r0 + j * (kThreads / kTileHeads);
     const bool there = p < parts && c0 < cols;
-    pm[j] = there ? all[p * part_size + c0] : -INFINITY;
-    pl[j] = there ? all[p * part_size + kTileHeads + c0] : 0.f;
+    const f32x2 v = there ? shared_load(all + p * part_size + 2 * c0) : f32x2{-INFINITY, 0.f};
+    pm[j] = v[0];
+    pl[j] = v[1];
   }
 #pragma unroll
   for (int j = 0; j < kEach; ++j) top = fmaxf(top, pm[j]);
@@ -210,12 +257,12 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A)
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kThreads / kTileHeads; ++r) top = fmaxf(top, some[r][c0]);
-  const float from = top == -INFINITY ? 0.f : top;
+  const float base = top == -INFINITY ? 0.f : top;
   float weight = 0.f;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     const int p = r0 + j * (kThreads / kTileHeads);
-    const float f = exp2_fast(pm[j] - from);
+    const float f = exp2_fast(pm[j] - base);
     weight += f * pl[j];
     if (p < parts) factor[p * kTileHeads + c0] = f;
   }
@@ -242,13 +289,16 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A)
       const float* from_part = all + 2 * kTileHeads + 4 * i;
       int p = mine;
       for (; p + 7 * share < parts; p += 8 * share) {
-        f32x4 v[8];
+        f32x2 v[16];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const f32x4*>(from_part + (p + j * share) * part_size);
+        for (int j = 0; j < 16; ++j) v[j] = shared_load(from_part + (p + j / 2 * share) * part_size + j % 2 * 2);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum += factor[(p + j * share) * kTileHeads + c] * v[j];
+        for (int j = 0; j < 8; ++j) sum += factor[(p + j * share) * kTileHeads + c] * f32x4{v[2 * j][0], v[2 * j][1], v[2 * j + 1][0], v[2 * j + 1][1]};
       }
-      for (; p < parts; p += share) sum += factor[p * kTileHeads + c] * *reinterpret_cast<const f32x4*>(from_part + p * part_size);
+      for (; p < parts; p += share) {
+        const f32x2 u = shared_load(from_part + p * part_size), v = shared_load(from_part + p * part_size + 2);
+        sum += factor[p * kTileHeads + c] * f32x4{u[0], u[1], v[0], v[1]};
+      }
     }
     if (share > 1) {   // quads < kThreads: one turn of the loop
       __syncthreads();
@@ -261,13 +311,27 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(const DecodeArgs A)
   }
 }
 
+template <bool BF16, int D>
+void launch_dim(const DecodeArgs& a, hipStream_t s) {
+  // Workgroups go to the 8 XCDs in turn: with the heads first every XCD has as much of every sequence, whatever its length (parts
+  // first, and 8 of them: the XCD of the last parts had nothing where sequences were short; 61 ragged ones 165 us, 77 so).
+  const dim3 grid(a.a.c.kv_heads * a.plan.tiles, a.a.c.n_seqs, a.plan.parts);
+  const bool whole = a.a.c.page_shift <= 5;
+  if (a.plan.waves == 8) {
+    if (whole) decode_kernel<BF16, D, true, 8><<<grid, 512, 0, s>>>(a);
+    else decode_kernel<BF16, D, false, 8><<<grid, 512, 0, s>>>(a);
+  } else {
+    if (whole) decode_kernel<BF16, D, true, 4><<<grid, 256, 0, s>>>(a);
+    else decode_kernel<BF16, D, false, 4><<<grid, 256, 0, s>>>(a);
+  }
+}
+
 template <bool BF16>
 void launch_type(const DecodeArgs& a, int head_dim, hipStream_t s) {
-  const dim3 grid(a.plan.parts, a.a.c.kv_heads * a.plan.tiles, a.a.c.n_seqs);
-  if (head_dim == 64) decode_kernel<BF16, 64><<<grid, 64 * kWaves, 0, s>>>(a);
-  else if (head_dim == 96) decode_kernel<BF16, 96><<<grid, 64 * kWaves, 0, s>>>(a);
-  else if (head_dim == 128) decode_kernel<BF16, 128><<<grid, 64 * kWaves, 0, s>>>(a);
-  else decode_kernel<BF16, 256><<<grid, 64 * kWaves, 0, s>>>(a);
+  if (head_dim == 64) launch_dim<BF16, 64>(a, s);
+  else if (head_dim == 96) launch_dim<BF16, 96>(a, s);
+  else if (head_dim == 128) launch_dim<BF16, 128>(a, s);
+  else launch_dim<BF16, 256>(a, s);
 }
 
 }  // namespace

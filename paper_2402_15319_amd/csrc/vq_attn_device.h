@@ -40,10 +40,9 @@ __device__ __forceinline__ void rows_of(const CacheArgs& c, int s, int* first, i
   *last = b;
 }
 
-// Page number j of sequence s, moved into the cache where the table holds another.
-__device__ __forceinline__ int page_inside(const CacheArgs& c, int s, int j) {
-  const uint32_t p = (uint32_t)c.table[(int64_t)s * c.table_width + j];
-  return (int)(p < (uint32_t)c.n_pages ? p : (uint32_t)c.n_pages - 1);
+// A page number from a table, moved into the cache where it lies outside.
+__device__ __forceinline__ int page_inside(const CacheArgs& c, int page) {
+  return (int)((uint32_t)page < (uint32_t)c.n_pages ? (uint32_t)page : (uint32_t)c.n_pages - 1);
 }
 
 // Eight values of the cache's type, the share of a lane in an operand of a matrix instruction.
@@ -66,10 +65,24 @@ template <bool BF16> __device__ __forceinline__ u32x4 pack8(f32x8 p) {
   else return __builtin_bit_cast(u32x4, __builtin_convertvector(p, f16x8));
 }
 
+// What one workgroup hands to another of the same launch goes past the caches that only some of the XCDs see: accesses of agent
+// scope, two values at a time, and before the word that says so the stores' completion.  (Fences of agent scope would do the
+// same for ordinary accesses, but write back and drop the XCD's whole L2: 24 sequences of 2,000 to 4,096 tokens in two parts, 1,536
+// workgroups, took 802 us with them and 240 us in one part.)
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void shared_store(float* p, float a, float b) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, f32x2{a, b}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 shared_load(const float* p) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ __forceinline__ void shared_stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp
 
-// Weights are exp2(x - m) with m the running maximum less this much: in fp16 a weight of 2^-14 and less would lose bits, so
-// the largest is 2^kLift there.  It cancels in out and in lse.
-template <bool BF16> constexpr float kLift = BF16 ? 0.f : 8.f;
+// Weights are exp2(x - m) with m a maximum less kLift: in fp16 weights below 2^-14 lose bits, so the largest start from 2^kLift
+// there.  It cancels in out and in lse.  m is left as it is until a logit is more than kSlack above the maximum it was taken from.
+template <bool BF16> constexpr float kLift = BF16 ? 0.f : 6.f;
+constexpr float kSlack = 8.f;
 
 }  // namespace vq

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(64) void attn_plain_kernel(const AttnArgs a, int he
   float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   for (int j0 = 0; j0 < n; j0 += 64) {
     const int j = j0 + lane;
-    const int page = page_inside(a.c, s, (j < n ? j : n - 1) >> a.c.page_shift);
+    const int page = page_inside(a.c, a.c.table[(int64_t)s * a.c.table_width + ((j < n ? j : n - 1) >> a.c.page_shift)]);
     const int64_t base = ((int64_t)page * a.c.kv_heads + h / a.group) * size * head_dim;
     float x = -INFINITY;
     if (j < n) {

@@ -58,6 +58,7 @@ hipError_t launch_attn_decode(const DecodeArgs& d, int head_dim, bool, hipStream
   REQUIRE(!a.c.q_start && a.c.n_seqs == a.c.n_tokens);
   // every token in a part, every query head in a tile, no part that the longest sequence leaves empty
   REQUIRE(p.chunk >= 128 && p.chunk % 128 == 0 && p.parts >= 1 && p.parts <= kMostParts && (long long)p.chunk * p.parts >= a.c.max_len);
+  REQUIRE(p.waves == 4 || (p.waves == 8 && p.parts == 1));
   REQUIRE(p.parts == 1 || (long long)p.chunk * (p.parts - 1) < a.c.max_len);
   REQUIRE((long long)p.chunk + a.c.max_len < 2147483647 - 1024);
   REQUIRE(p.cols >= 1 && p.cols <= kTileHeads && p.tiles * kTileHeads >= a.group && p.cols == (a.group < kTileHeads ? a.group : kTileHeads));
