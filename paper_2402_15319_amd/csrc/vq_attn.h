@@ -63,6 +63,10 @@ struct DecodeArgs {
 // What a part leaves: 16 maxima, 16 sums of weights, and sums over the values for each head of the tile.
 __host__ __device__ inline size_t part_floats(const DecodePlan& p, int head_dim) { return 2 * kTileHeads + (size_t)p.cols * head_dim; }
 
+// vq_attn_prompt: (new token, query head) pairs that a workgroup takes, and workgroups of a launch at most.
+constexpr int kPromptRows = 128;
+constexpr int64_t kPromptMostWorkgroups = 1 << 23;
+
 // Pages copied by one launch: every pair in every buffer.  No page of a launch is written twice, or read and written.
 constexpr int kCopyBuffers = 128, kCopyPairs = 320;
 struct CopyArgs {
@@ -77,5 +81,6 @@ hipError_t launch_append(const AppendArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_copy(const CopyArgs& a, hipStream_t s);
 hipError_t launch_attn_decode(const DecodeArgs& a, int head_dim, bool bf16, hipStream_t s);
 hipError_t launch_attn_prompt(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_attn_prompt_256(const AttnArgs& a, bool bf16, hipStream_t s);
 
 }  // namespace vq

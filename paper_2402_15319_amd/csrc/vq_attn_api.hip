@@ -32,6 +32,7 @@ int check_batch_sizes(const vq_attn_desc& d, const vq_attn_batch* b) {
   if (!b) return VQ_ERR_NULL;
   if (b->n_seqs < 1 || b->n_seqs > 65535 || b->n_tokens < 1 || b->table_width < 1 || b->max_len < 0 || b->max_len > kMostLen) return VQ_ERR_BAD_ARG;
   if ((int64_t)b->max_len > (int64_t)b->table_width * d.page_size) return VQ_ERR_BAD_ARG;
+  if ((int64_t)b->n_tokens * d.heads / kPromptRows + (int64_t)b->n_seqs * d.kv_heads > kPromptMostWorkgroups) return VQ_ERR_BAD_ARG;
   return VQ_OK;
 }
 

@@ -59,6 +59,14 @@ template <bool BF16> __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f
   else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// 32 x 32 += 32 x 16 . 16 x 32.  Lane L holds row (a) or column (b) L % 32 at k = 8 (L / 32) .. + 7, and of the result column
+// L % 32 at rows 8 (i / 4) + 4 (L / 32) + i % 4, i < 16.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <bool BF16> __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
 // Eight weights rounded to the cache's type.
 template <bool BF16> __device__ __forceinline__ u32x4 pack8(f32x8 p) {
   if constexpr (BF16) return __builtin_bit_cast(u32x4, __builtin_convertvector(p, bf16x8));
@@ -77,6 +85,17 @@ __device__ __forceinline__ f32x2 shared_load(const float* p) {
   return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 __device__ __forceinline__ void shared_stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// 64 lanes x 16 bytes (base + voff, voff per lane) into 1 KB of LDS from byte address lds on.  No register takes the data; the
+// wave's vmcnt counts it, the compiler does not.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
+}
+
+// The wave's loads into LDS have arrived and its reads from LDS have been answered, then the workgroup's other waves'.
+__device__ __forceinline__ void lds_turn() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp
 

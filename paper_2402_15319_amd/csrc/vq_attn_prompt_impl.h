@@ -1,0 +1,257 @@
+// Causal attention of any number of new tokens of every sequence over the paged cache: the kernel.
+#pragma once
+#include <type_traits>
+
+#include "vq_attn_device.h"
+
+namespace vq {
+namespace {
+
+constexpr int kWaves = 4, kRows = kPromptRows, kTokens = 64;   // rows of a workgroup's tile; tokens of a step
+static_assert(kRows == 32 * kWaves, "32 rows a wave");
+
+// 16-byte pieces of a row of K in LDS change places so that 16 rows' pieces of one number lie in different banks: piece p of row r
+// lies where piece p ^ k_turn(r) would.
+template <int D> __device__ __forceinline__ int k_turn(int r) {
+  return D % 128 == 0 ? r & 15 : D == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
+}
+
+// One workgroup: 128 rows of one sequence and one key/value head, a row being a (new token, query head of the group) pair, 32 a
+// wave, and all tokens that they attend, 64 at a time.
+//   S^T = K Q^T, O^T += V^T P^T, 32 x 32 x 16: a lane has one row's logits (half of a step's), weights and sums, so that a row's
+//   maximum and sum need the other half-wave only, and P goes from the first product's registers into the second's as
+//   it is: row m of the first operand is token m with bits 2 and 3 exchanged, which leaves a lane with eight successive tokens.
+// K and V^T of a step come into LDS past the registers, each wave 16 tokens of both (one page), while the step before is
+// worked on.
+template <bool BF16, int D>
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(const AttnArgs a) {
+  constexpr int KS = D / 16, DT = D / 32, kLoads = D / 32;     // loads of a wave for its 16 tokens' K, and for their V
+  constexpr int kHalf = kTokens * D * 2, kStep = 2 * kHalf;    // bytes of K, or V, of a step
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kStep];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
+  // The heads are neighbours, and so are on the 8 XCDs in turn: those of an XCD keep to their keys and values.  Of the tiles the last come
+  // first: they attend most.
+  const int slots = gridDim.x / a.c.kv_heads, kvh = blockIdx.x % a.c.kv_heads, slot = slots - 1 - blockIdx.x / a.c.kv_heads;
+  const int group = a.group;
+
+  // The sequence: its tiles start at slot floor(first row / 128) + its number, which leaves room for a last tile that is not full.
+  int s = -1;
+  for (int base = 0; base < a.c.n_seqs; base += 64) {
+    const int i = base + lane;
+    int at = 0x7fffffff;
+    if (i < a.c.n_seqs) {
+      int first = a.c.q_start ? a.c.q_start[i] : i;
+      first = first < 0 ? 0 : first < a.c.n_tokens ? first : a.c.n_tokens;
+      at = first * group / kRows + i;
+    }
+    const int before = __popcll(__ballot(at <= slot));
+    s += before;
+    if (before < 64) break;
+  }
+  s = __builtin_amdgcn_readfirstlane(s < 0 ? 0 : s);
+  int first, last;
+  rows_of(a.c, s, &first, &last);
+  const int n = last - first, rows = n * group, row0 = (slot - (first * group / kRows + s)) * kRows;
+  if (row0 < 0 || row0 >= rows) return;
+  const int len = cached_tokens(a.c, s), behind = len - n;   // new token i has position behind + i
+  const int row = row0 + 32 * wave + col, row_in = row < rows ? row : rows - 1;
+  const int token = row_in / group, head = kvh * group + (row_in - token * group);
+  const int pos = behind + token;
+  const int wave_row = row0 + 32 * wave;
+  const int wave_last = wave_row < rows ? behind + ((wave_row + 31 < rows ? wave_row + 31 : rows - 1) / group) : -1;   // highest position
+  const int wave_first = behind + wave_row / group;
+  const int most = behind + ((row0 + kRows - 1 < rows ? row0 + kRows - 1 : rows - 1) / group);
+  const int steps = most < 0 ? 0 : most / kTokens + 1;
+
+  u32x4 q[KS];
+  {
+    const uint16_t* from = a.q + (int64_t)(first + token) * a.qs.token + head * a.qs.head;
+    if (a.qs.dim == 1 && ((a.qs.token | a.qs.head) & 7) == 0) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) q[k] = *reinterpret_cast<const u32x4*>(from + 16 * k + 8 * half);
+    } else {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int64_t d = 16 * k + 8 * half + 2 * i;
+          q[k][i] = from[d * a.qs.dim] | (uint32_t)from[(d + 1) * a.qs.dim] << 16;
+        }
+    }
+  }
+
+#pragma unroll
+  for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));   // here, or the compiler waits for them in the loop, and with them for its loads
+
+  // Loads: the wave's tokens are 16 wave .. + 15 of the step.  K: rows of D values, their pieces turned; V^T: for each dimension two
+  // pieces of eight tokens, exchanged where bit 3 of the dimension is set.
+  const int shift = a.c.page_shift, mask = (1 << shift) - 1, last_page = len > 0 ? (len - 1) >> shift : 0;
+  uint32_t k_off[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int at = 64 * j + lane, r = at / (D / 8), p = at % (D / 8);
+    k_off[j] = (r * D + (p ^ k_turn<D>(r)) * 8) * 2;
+  }
+  const uint32_t v_off = (((lane >> 1) << shift) + 8 * ((lane & 1) ^ ((lane >> 4) & 1))) * 2;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
+  const int32_t* table = a.c.table + (int64_t)s * a.c.table_width;
+  int pages = 0;   // lane i: the wave's page in step i (mod 64) of the 64 that are being loaded
+  auto load = [&](int step) {
+    if ((step & 63) == 0) {
+      const int j = ((step + lane) * kTokens + 16 * wave) >> shift;
+      pages = table[j < last_page ? j : last_page];
+    }
+    const int page = page_inside(a.c, __builtin_amdgcn_readlane(pages, step & 63));
+    const int in = (step * kTokens + 16 * wave) & mask;
+    const int64_t page_head = ((int64_t)page * a.c.kv_heads + kvh) * ((int64_t)D << shift);
+    const uint16_t* k = a.k_pages + page_head + in * D;
+    const uint16_t* v = a.v_pages + page_head + in;
+    const uint32_t to = lds0 + (step & 1) * kStep + wave * (kHalf / kWaves);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_to_lds(k, k_off[j], to + 1024 * j);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_to_lds(v + ((int64_t)(32 * j) << shift), v_off, to + kHalf + 1024 * j);
+  };
+
+  float m = -INFINITY, from = 0.f, l = 0.f;   // as in the kernel of one new token
+  f32x16 o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+  const int k_row = (col & 0x13) | (col & 4) << 1 | (col & 8) >> 1;
+
+  auto work = [&](int step, auto masked_) {
+    constexpr bool masked = decltype(masked_)::value;
+    const char* kt = lds + (step & 1) * kStep;
+    const char* vt = kt + kHalf;
+    f32x16 x[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[t][j] = 0.f;
+      const int r = 32 * t + k_row;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (r * (D / 8) + ((2 * k + half) ^ k_turn<D>(r))) * 16);
+        x[t] = mfma32<BF16>(f, q[k], x[t]);
+      }
+    }
+    const int rel = pos - step * kTokens - 8 * half;   // tokens of the lane up to here are attended
+    if constexpr (masked) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[t][j] = 32 * t + 16 * (j >> 3) + (j & 7) <= rel ? x[t][j] : -INFINITY;
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) top = fmaxf(top, x[t][j]);
+    if (__any(top * a.scale_log2 > m + (kLift<BF16> + kSlack))) {
+      top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+      const float old = m;
+      m = fmaxf(m, top - kLift<BF16>);
+      from = m == -INFINITY ? 0.f : m;
+      const float shrink = exp2_fast(old - from);
+      l *= shrink;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= shrink;
+    }
+    u32x4 p[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      f32x8 w;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = exp2_fast(fmaf(x[c >> 1][8 * (c & 1) + j], a.scale_log2, -from));
+        l += w[j];
+      }
+      p[c] = pack8<BF16>(w);
+    }
+    const char* v_at = vt + col * 32 + (half ^ ((col >> 3) & 1)) * 16;
+    if constexpr (masked) {
+      // A weight of 0 must not meet a value that is no number: tokens behind the last one are cleared, and what else there is
+      // of them is left out of the product and given afterwards to the rows that attend it.
+      constexpr uint32_t kExp = BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = BF16 ? 0x00800080u : 0x04000400u;
+      uint32_t odd = 0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int rest = len - step * kTokens - 16 * c - 8 * half;
+        u32x4 keep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) keep[j] = (2 * j < rest ? 0xffffu : 0u) | (2 * j + 1 < rest ? 0xffff0000u : 0u);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          u32x4 f = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32) & keep;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t t = ((f[j] & kExp) + kOne) & 0x80008000u;   // the halves with a full exponent
+            odd |= t;
+            f[j] &= ~((t >> 15) * 0xffffu);
+          }
+          o[i] = mfma32<BF16>(f, p[c], o[i]);
+        }
+      }
+      if (__any(odd)) {
+        for (int j = 0; j < kTokens; ++j) {
+          const bool mine = step * kTokens + j <= pos;
+#pragma unroll
+          for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int d = 32 * i + 8 * (e >> 2) + 4 * half + (e & 3);
+              const float v = to_f32<BF16>(*reinterpret_cast<const uint16_t*>(vt + ((j >> 4) * D + d) * 32 + (((j >> 3) ^ (e >> 2)) & 1) * 16 + (j & 7) * 2));
+              if (mine && !(fabsf(v) < INFINITY)) o[i][e] += v;
+            }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] = mfma32<BF16>(*reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32), p[c], o[i]);
+    }
+  };
+
+  // First the steps whose tokens all of the wave's rows attend.
+  const int whole = wave_row < rows && wave_first >= 0 ? (wave_first + 1) / kTokens : 0;
+  if (steps > 0) load(0);
+  int step = 0;
+  for (; step < whole; ++step) {
+    lds_turn();
+    if (step + 1 < steps) load(step + 1);
+    work(step, std::false_type());
+  }
+  for (; step < steps; ++step) {
+    lds_turn();
+    if (step + 1 < steps) load(step + 1);
+    if (step * kTokens <= wave_last) work(step, std::true_type());
+  }
+
+  l += __shfl_xor(l, 32);
+  if (wave_row >= rows) return;
+  const bool any = pos >= 0;
+  const float scale = any ? 1.f / l : 0.f;
+  if (row >= rows) return;
+  uint16_t* to = a.out + (int64_t)(first + token) * a.os.token + head * a.os.head;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int64_t d = 32 * i + 8 * (j >> 2) + 4 * half + (j & 3);
+      to[d * a.os.dim] = from_f32<BF16>(any ? o[i][j] * scale : 0.f);
+    }
+  if (a.lse && half == 0) a.lse[(int64_t)(first + token) * a.heads + head] = any ? (m + __log2f(l)) * 0.693147180559945f : -INFINITY;
+}
+
+template <bool BF16, int D>
+hipError_t launch_prompt(const AttnArgs& a, hipStream_t s) {
+  const int64_t slots = (int64_t)a.c.n_tokens * a.group / kPromptRows + a.c.n_seqs;
+  prompt_kernel<BF16, D><<<(unsigned)(a.c.kv_heads * slots), 64 * kWaves, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace vq

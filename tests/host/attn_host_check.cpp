@@ -73,6 +73,8 @@ hipError_t launch_attn_decode(const DecodeArgs& d, int head_dim, bool, hipStream
 
 hipError_t launch_attn_prompt(const AttnArgs& a, int head_dim, bool, hipStream_t) {
   check_attn(a, head_dim);
+  REQUIRE((long long)a.c.n_tokens * a.group + kPromptRows < 2147483647);   // rows of a key/value head
+  REQUIRE(((long long)a.c.n_tokens * a.group / kPromptRows + a.c.n_seqs) * a.c.kv_heads * 256 < 4294967296ll);
   return hipSuccess;
 }
 }  // namespace vq
@@ -131,6 +133,10 @@ static void calls(std::mt19937& rng) {
     b.page_table = (const int32_t*)at(2);
     b.q_start = one_each ? nullptr : (const int32_t*)at(3);
     size_t n = 0;
+    if ((long long)b.n_tokens * d.heads / 128 + (long long)b.n_seqs * d.kv_heads > 1 << 23) {
+      REQUIRE(vq_attn_workspace_bytes(&d, &b, &n) == VQ_ERR_BAD_ARG);
+      continue;
+    }
     REQUIRE(vq_attn_workspace_bytes(&d, &b, &n) == VQ_OK && n >= 16);
     vq::g_workspace = n;
     const vq_strides wide = {(int64_t)d.heads * d.head_dim, d.head_dim, 1};
