@@ -7,6 +7,7 @@ built, importing the binding's functions raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import struct
@@ -129,7 +130,7 @@ def lib() -> ctypes.CDLL:
         L.vq_cache_append.restype = i32
         L.vq_cache_append.argtypes = [ap, bp, vp, st, vp, st, vp, vp, vp]
         L.vq_cache_copy.restype = i32
-        L.vq_cache_copy.argtypes = [ap, i32, ctypes.POINTER(vp), i32, ctypes.POINTER(ctypes.c_int32), vp]
+        L.vq_cache_copy.argtypes = [ap, i32, vp, i32, vp, vp]   # two host arrays
         L.vq_attn_workspace_bytes.restype = i32
         L.vq_attn_workspace_bytes.argtypes = [ap, bp, sz]
         for name in ("vq_attn_decode", "vq_attn_prompt"):
@@ -361,11 +362,12 @@ def vq_cache_append(desc: VQAttnDesc, batch: AttnBatch, k, v, k_pages, v_pages, 
 
 def vq_cache_copy(desc: VQAttnDesc, buffers, from_to, stream=None) -> None:
     """buffers: K and V buffers; from_to: (page, page) pairs, copied one after another in every buffer."""
-    flat = [int(p) for pair in from_to for p in pair]
-    if len(flat) != 2 * len(from_to):
-        raise ValueError("vq_cache_copy: from_to is a list of pairs")
-    _check(lib().vq_cache_copy(desc, len(buffers), (ctypes.c_void_p * len(buffers))(*[_ptr(b) for b in buffers]), len(from_to),
-                               (ctypes.c_int32 * len(flat))(*flat), _stream(stream)), "vq_cache_copy")
+    try:
+        flat = array.array("i", [p for a, b in from_to for p in (a, b)])
+    except (ValueError, TypeError, OverflowError) as e:
+        raise ValueError("vq_cache_copy: from_to is a list of pairs of page numbers") from e
+    at = array.array("Q", [b if isinstance(b, int) else b.data_ptr() for b in buffers])
+    _check(lib().vq_cache_copy(desc, len(at), at.buffer_info()[0], len(flat) // 2, flat.buffer_info()[0], _stream(stream)), "vq_cache_copy")
 
 
 def vq_attn_workspace_bytes(desc: VQAttnDesc, batch: AttnBatch) -> int:

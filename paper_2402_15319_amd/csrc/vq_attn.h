@@ -63,22 +63,25 @@ struct DecodeArgs {
 // What a part leaves: 16 maxima, 16 sums of weights, and sums over the values for each head of the tile.
 __host__ __device__ inline size_t part_floats(const DecodePlan& p, int head_dim) { return 2 * kTileHeads + (size_t)p.cols * head_dim; }
 
-// vq_attn_prompt: (new token, query head) pairs that a workgroup takes, and workgroups of a launch at most.
+// vq_attn_prompt: (new token, query head) pairs that a workgroup takes, and workgroups of a launch at most, which bounds those of an
+// append too (2^32 threads for each dimension of a grid).
 constexpr int kPromptRows = 128;
-constexpr int64_t kPromptMostWorkgroups = 1 << 23;
+constexpr int64_t kPromptMostWorkgroups = 1 << 20;
 
 // Pages copied by one launch: every pair in every buffer.  No page of a launch is written twice, or read and written.
-constexpr int kCopyBuffers = 128, kCopyPairs = 320;
-struct CopyArgs {
+constexpr int kCopyBuffers = 128, kCopyPairs = 1024, kCopyFew = 64;
+template <int PAIRS>
+struct CopyArgsOf {
   uint64_t page_bytes;
-  int32_t n_buffers, n_pairs;
+  int32_t n_buffers, n_pairs, pieces, reserved;   // pieces: workgroups for a page
   void* buffer[kCopyBuffers];
-  int32_t from_to[kCopyPairs][2];
+  int32_t from_to[PAIRS][2];
 };
-static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
+typedef CopyArgsOf<kCopyPairs> CopyArgs;
+static_assert(sizeof(CopyArgs) <= 16384, "kernel arguments");
 
 hipError_t launch_append(const AppendArgs& a, int head_dim, hipStream_t s);
-hipError_t launch_copy(const CopyArgs& a, hipStream_t s);
+hipError_t launch_copy(CopyArgs& a, hipStream_t s);
 hipError_t launch_attn_decode(const DecodeArgs& a, int head_dim, bool bf16, hipStream_t s);
 hipError_t launch_attn_prompt(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s);
 hipError_t launch_attn_prompt_256(const AttnArgs& a, bool bf16, hipStream_t s);

@@ -216,16 +216,17 @@ int vq_cache_copy(const vq_attn_desc* desc, int n_buffers, void* const* buffers,
     if (from_to[i] < 0 || from_to[i] >= desc->n_pages) return VQ_ERR_BAD_ARG;
   // Launches of one stream follow one another, so what depends on an earlier pair starts a new one.  The pages of a launch
   // are held in a small hash table (open addressing, at most half full): 1 read, 2 written.
-  constexpr int kSlots = 2048;
+  constexpr int kSlots = 4096;
   static_assert(kSlots >= 4 * kCopyPairs, "half full at most");
   CopyArgs a;
+  a.reserved = 0;
   a.page_bytes = (uint64_t)desc->kv_heads * desc->page_size * desc->head_dim * 2;
   for (int first = 0; first < n_pairs;) {
     int32_t page[kSlots];
     uint8_t use[kSlots];
     memset(use, 0, sizeof(use));
     const auto slot = [&](int32_t p) {
-      uint32_t h = ((uint32_t)p * 2654435761u) >> 21;
+      uint32_t h = ((uint32_t)p * 2654435761u) >> 20;
       while (use[h] && page[h] != p) h = (h + 1) & (kSlots - 1);
       return h;
     };

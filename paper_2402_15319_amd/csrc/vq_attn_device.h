@@ -14,15 +14,28 @@ template <bool BF16> __device__ __forceinline__ uint16_t from_f32(float f) {
   else return __builtin_bit_cast(uint16_t, (_Float16)f);
 }
 
-// The sequence that owns new token t: the last one that starts at or before it.
-__device__ __forceinline__ int sequence_of(const CacheArgs& c, int t) {
-  if (!c.q_start) return t;
-  int lo = 0, hi = c.n_seqs;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (c.q_start[mid] <= t) lo = mid; else hi = mid;
+// Work is handed out in tiles of `unit` rows of a sequence (a new token counts `each` rows), at most floor(rows / unit) + extra of
+// them.  Those of sequence i start at slot floor(first row / unit) + extra * i, which leaves room for the last ones of the sequences before;
+// this is the sequence of a slot and the slot's number among its own.  A wave looks at 64 sequences at a time.
+struct Tile { int sequence, number; };
+__device__ __forceinline__ Tile tile_of(const CacheArgs& c, int slot, int each, int unit, int extra) {
+  const int lane = threadIdx.x & 63;
+  int s = 0, start = 0;
+  for (int base = 0; base < c.n_seqs; base += 64) {
+    const int i = base + lane;
+    int at = 0x7fffffff;
+    if (i < c.n_seqs) {
+      int first = c.q_start ? c.q_start[i] : i;
+      first = first < 0 ? 0 : first < c.n_tokens ? first : c.n_tokens;
+      at = first * each / unit + extra * i;
+    }
+    const int before = __popcll(__ballot(at <= slot));
+    if (before == 0) break;   // never in the first turn: sequence 0 starts at slot 0 where q_start is as it should be
+    s = base + before - 1;
+    start = __builtin_amdgcn_readlane(at, before - 1);
+    if (before < 64) break;
   }
-  return lo;
+  return {s, slot - start};
 }
 
 // Tokens in the cache of sequence s: what the table can list at most.

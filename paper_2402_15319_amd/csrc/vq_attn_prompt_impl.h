@@ -34,25 +34,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
   const int slots = gridDim.x / a.c.kv_heads, kvh = blockIdx.x % a.c.kv_heads, slot = slots - 1 - blockIdx.x / a.c.kv_heads;
   const int group = a.group;
 
-  // The sequence: its tiles start at slot floor(first row / 128) + its number, which leaves room for a last tile that is not full.
-  int s = -1;
-  for (int base = 0; base < a.c.n_seqs; base += 64) {
-    const int i = base + lane;
-    int at = 0x7fffffff;
-    if (i < a.c.n_seqs) {
-      int first = a.c.q_start ? a.c.q_start[i] : i;
-      first = first < 0 ? 0 : first < a.c.n_tokens ? first : a.c.n_tokens;
-      at = first * group / kRows + i;
-    }
-    const int before = __popcll(__ballot(at <= slot));
-    s += before;
-    if (before < 64) break;
-  }
-  s = __builtin_amdgcn_readfirstlane(s < 0 ? 0 : s);
+  const Tile tile = tile_of(a.c, slot, group, kRows, 1);
+  const int s = tile.sequence;
   int first, last;
   rows_of(a.c, s, &first, &last);
-  const int n = last - first, rows = n * group, row0 = (slot - (first * group / kRows + s)) * kRows;
-  if (row0 < 0 || row0 >= rows) return;
+  const int n = last - first, rows = n * group, row0 = tile.number * kRows;
+  if (row0 >= rows) return;
   const int len = cached_tokens(a.c, s), behind = len - n;   // new token i has position behind + i
   const int row = row0 + 32 * wave + col, row_in = row < rows ? row : rows - 1;
   const int token = row_in / group, head = kvh * group + (row_in - token * group);
@@ -126,16 +113,31 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
     const char* kt = lds + (step & 1) * kStep;
     const char* vt = kt + kHalf;
     f32x16 x[2];
+    u32x4 f[4 * DT];   // an operand's fragments, all asked for before the first is used (KS = 2 DT)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int r = 32 * t + k_row;
+        f[2 * k + t] = *reinterpret_cast<const u32x4*>(kt + (r * (D / 8) + ((2 * k + half) ^ k_turn<D>(r))) * 16);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int j = 0; j < 16; ++j) x[t][j] = 0.f;
-      const int r = 32 * t + k_row;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (r * (D / 8) + ((2 * k + half) ^ k_turn<D>(r))) * 16);
-        x[t] = mfma32<BF16>(f, q[k], x[t]);
-      }
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) x[t] = mfma32<BF16>(f[2 * k + t], q[k], x[t]);
+    __builtin_amdgcn_sched_barrier(0);
+    const char* v_at = vt + col * 32 + (half ^ ((col >> 3) & 1)) * 16;
+    if constexpr (!masked) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < DT; ++i) f[c * DT + i] = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32);
+      __builtin_amdgcn_sched_barrier(0);
     }
     const int rel = pos - step * kTokens - 8 * half;   // tokens of the lane up to here are attended
     if constexpr (masked) {
@@ -170,7 +172,6 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
       }
       p[c] = pack8<BF16>(w);
     }
-    const char* v_at = vt + col * 32 + (half ^ ((col >> 3) & 1)) * 16;
     if constexpr (masked) {
       // A weight of 0 must not meet a value that is no number: tokens behind the last one are cleared, and what else there is
       // of them is left out of the product and given afterwards to the rows that attend it.
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int i = 0; i < DT; ++i) o[i] = mfma32<BF16>(*reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32), p[c], o[i]);
+        for (int i = 0; i < DT; ++i) o[i] = mfma32<BF16>(f[c * DT + i], p[c], o[i]);
     }
   };
 

@@ -32,10 +32,11 @@ hipError_t launch_append(const AppendArgs& a, int head_dim, hipStream_t) {
   ++g_launches;
   check_cache(a.c);
   REQUIRE(head_dim % 32 == 0 && head_dim <= 256);
+  REQUIRE((a.c.n_tokens / 64 + 2ll * a.c.n_seqs) * a.c.kv_heads * 512 <= 4294967295ll);
   return hipSuccess;
 }
 
-hipError_t launch_copy(const CopyArgs& a, hipStream_t) {
+hipError_t launch_copy(CopyArgs& a, hipStream_t) {
   ++g_launches;
   REQUIRE(a.n_pairs >= 1 && a.n_pairs <= kCopyPairs && a.n_buffers >= 1 && a.n_buffers <= kCopyBuffers && a.page_bytes % 16 == 0);
   for (int b = 0; b < a.n_buffers; ++b)   // in another order than the pairs': they must not depend on one another
@@ -84,8 +85,8 @@ static void* at(uintptr_t i) { return reinterpret_cast<void*>(i << 20); }   // n
 static void copies(std::mt19937& rng) {
   vq_attn_desc d = {1, 1, 64, 16, 1, VQ_F16, 0.f, 0};
   for (int round = 0; round < 60; ++round) {
-    d.n_pages = 2 + rng() % (round < 40 ? 30 : 900);
-    const int n_buffers = round % 20 == 0 ? 1 + vq::kCopyBuffers + rng() % 3 : 1 + rng() % 3, n_pairs = 1 + rng() % (round < 40 ? 60 : 1200);
+    d.n_pages = 2 + rng() % (round < 40 ? 30 : round < 50 ? 900 : 6000);
+    const int n_buffers = round % 20 == 0 ? 1 + vq::kCopyBuffers + rng() % 3 : 1 + rng() % 3, n_pairs = 1 + rng() % (round < 40 ? 60 : 3000);
     const size_t page = 64 * 16;   // 16-bit values
     std::vector<std::vector<uint16_t>> got(n_buffers, std::vector<uint16_t>(d.n_pages * page)), want;
     for (auto& b : got)
@@ -133,7 +134,7 @@ static void calls(std::mt19937& rng) {
     b.page_table = (const int32_t*)at(2);
     b.q_start = one_each ? nullptr : (const int32_t*)at(3);
     size_t n = 0;
-    if ((long long)b.n_tokens * d.heads / 128 + (long long)b.n_seqs * d.kv_heads > 1 << 23) {
+    if ((long long)b.n_tokens * d.heads / 128 + (long long)b.n_seqs * d.kv_heads > 1 << 20) {
       REQUIRE(vq_attn_workspace_bytes(&d, &b, &n) == VQ_ERR_BAD_ARG);
       continue;
     }
