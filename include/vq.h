@@ -308,7 +308,7 @@ typedef struct vq_attn_desc {
 typedef struct vq_attn_batch {
   int32_t n_seqs;             /* sequences, [1, 65535]                                               */
   int32_t n_tokens;           /* new tokens of all sequences together (rows of q, k, v, out), >= 1;
-                                 n_tokens * heads / 128 + n_seqs * kv_heads is at most 2^20          */
+                                 n_tokens * heads / 128 + n_seqs * heads is at most 2^20             */
   int32_t table_width;        /* pages that a row of page_table lists, >= 1                          */
   int32_t max_len;            /* no kv_len is larger; [0, table_width * page_size], at most 2^29.
                                  Decides how the work is split; a larger kv_len is taken as max_len  */

@@ -65,8 +65,24 @@ __host__ __device__ inline size_t part_floats(const DecodePlan& p, int head_dim)
 
 // vq_attn_prompt: (new token, query head) pairs that a workgroup takes, and workgroups of a launch at most, which bounds those of an
 // append too (2^32 threads for each dimension of a grid).
-constexpr int kPromptRows = 128;
+constexpr int kPromptRows = 128, kPromptTokens = 64;   // tokens: of a step
 constexpr int64_t kPromptMostWorkgroups = 1 << 20;
+
+// How a call of vq_attn_prompt is split: slots for tiles of 128 rows of a sequence, a row being a (new token, query head) pair, and parts of
+// at most so many steps.  A tile has `heads` query heads of one key/value head: all of the group, row after row those of a token, or, by
+// head, 1, 2 or 4 with 32 successive tokens of one head to a wave.
+struct PromptPlan {
+  int64_t slots;
+  int32_t steps, parts;
+  int32_t heads, by_head;
+};
+struct PromptArgs {
+  AttnArgs a;
+  PromptPlan plan;
+  uint32_t* counter;   // [slots][heads / plan.heads]
+  float* part;         // [slots][heads / plan.heads][parts][prompt_part_floats]
+};
+inline size_t prompt_part_floats(int head_dim) { return kPromptRows * (4 + (size_t)head_dim); }
 
 // Pages copied by one launch: every pair in every buffer.  No page of a launch is written twice, or read and written.
 constexpr int kCopyBuffers = 128, kCopyPairs = 1024, kCopyFew = 64;
@@ -83,7 +99,7 @@ static_assert(sizeof(CopyArgs) <= 16384, "kernel arguments");
 hipError_t launch_append(const AppendArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_copy(CopyArgs& a, hipStream_t s);
 hipError_t launch_attn_decode(const DecodeArgs& a, int head_dim, bool bf16, hipStream_t s);
-hipError_t launch_attn_prompt(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s);
-hipError_t launch_attn_prompt_256(const AttnArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_attn_prompt(const PromptArgs& a, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_attn_prompt_256(const PromptArgs& a, bool bf16, hipStream_t s);
 
 }  // namespace vq

@@ -32,7 +32,7 @@ int check_batch_sizes(const vq_attn_desc& d, const vq_attn_batch* b) {
   if (!b) return VQ_ERR_NULL;
   if (b->n_seqs < 1 || b->n_seqs > 65535 || b->n_tokens < 1 || b->table_width < 1 || b->max_len < 0 || b->max_len > kMostLen) return VQ_ERR_BAD_ARG;
   if ((int64_t)b->max_len > (int64_t)b->table_width * d.page_size) return VQ_ERR_BAD_ARG;
-  if ((int64_t)b->n_tokens * d.heads / kPromptRows + (int64_t)b->n_seqs * d.kv_heads > kPromptMostWorkgroups) return VQ_ERR_BAD_ARG;
+  if ((int64_t)b->n_tokens * d.heads / kPromptRows + (int64_t)b->n_seqs * d.heads > kPromptMostWorkgroups) return VQ_ERR_BAD_ARG;
   return VQ_OK;
 }
 
@@ -121,12 +121,35 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   return p;
 }
 
-int attn_workspace(const vq_attn_desc& d, const vq_attn_batch& b, size_t* bytes) {
+constexpr int64_t kEnoughTiles = 512;   // workgroups
+constexpr int kLeastSteps = 8;          // of a part
+
+PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
+  PromptPlan p;
+  const int group = d.heads / d.kv_heads, by = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
+  p.by_head = (int64_t)b.n_tokens * by >= (int64_t)kPromptRows * b.n_seqs;   // the sequences' tokens fill such a tile
+  p.heads = p.by_head ? by : group;
+  p.slots = (int64_t)b.n_tokens * p.heads / kPromptRows + b.n_seqs;
+  const int64_t units = p.slots * (d.heads / p.heads), steps = b.max_len > 0 ? ((int64_t)b.max_len + kPromptTokens - 1) / kPromptTokens : 1;
+  int64_t parts = units < kEnoughTiles ? (kEnoughTiles + units - 1) / units : 1;
+  while (parts > 1 && parts * parts > steps) --parts;   // to join a part takes about as long as a step
+  int64_t per = (steps + parts - 1) / parts;
+  per = per < kLeastSteps ? kLeastSteps : per;
+  p.steps = (int32_t)per;
+  p.parts = (int32_t)((steps + per - 1) / per);
+  return p;
+}
+
+// Bytes of the workspace: the counters and what the parts leave, where there are several.
+size_t decode_workspace(const vq_attn_desc& d, const vq_attn_batch& b) {
   const DecodePlan p = decode_plan(d, b);
-  *bytes = 16;
-  if (b.n_tokens == b.n_seqs && p.parts > 1)
-    *bytes = kJoinCounters * sizeof(uint32_t) + (size_t)b.n_seqs * d.kv_heads * p.tiles * p.parts * part_floats(p, d.head_dim) * sizeof(float);
-  return VQ_OK;
+  if (p.parts <= 1) return 16;
+  return kJoinCounters * sizeof(uint32_t) + (size_t)b.n_seqs * d.kv_heads * p.tiles * p.parts * part_floats(p, d.head_dim) * sizeof(float);
+}
+size_t prompt_workspace(const vq_attn_desc& d, const vq_attn_batch& b) {
+  const PromptPlan p = prompt_plan(d, b);
+  if (p.parts <= 1) return 16;
+  return kJoinCounters * sizeof(uint32_t) + (size_t)p.slots * (d.heads / p.heads) * p.parts * prompt_part_floats(d.head_dim) * sizeof(float);
 }
 
 int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,
@@ -145,10 +168,7 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   if (st != VQ_OK) return st;
   st = check_strides(out_strides, batch->n_tokens, desc->heads, desc->head_dim, true, &a.os);
   if (st != VQ_OK) return st;
-  size_t need = 0;
-  st = attn_workspace(*desc, *batch, &need);
-  if (st != VQ_OK) return st;
-  if (workspace_bytes < need) return VQ_ERR_BAD_ARG;
+  if (workspace_bytes < (decode ? decode_workspace(*desc, *batch) : prompt_workspace(*desc, *batch))) return VQ_ERR_BAD_ARG;
   a.c = cache_args(*desc, *batch, decode);
   a.q = (const uint16_t*)q;
   a.k_pages = (const uint16_t*)k_pages;
@@ -159,7 +179,10 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   a.group = desc->heads / desc->kv_heads;
   a.scale_log2 = desc->scale * 1.44269504088896f;
   const bool bf16 = desc->dtype == VQ_BF16;
-  if (!decode) return hip_status(launch_attn_prompt(a, desc->head_dim, bf16, (hipStream_t)stream));
+  if (!decode) {
+    const PromptArgs prompt = {a, prompt_plan(*desc, *batch), (uint32_t*)workspace, (float*)workspace + kJoinCounters};
+    return hip_status(launch_attn_prompt(prompt, desc->head_dim, bf16, (hipStream_t)stream));
+  }
   both.plan = decode_plan(*desc, *batch);
   both.counter = (uint32_t*)workspace;
   both.part = (float*)workspace + kJoinCounters;
@@ -263,7 +286,9 @@ int vq_attn_workspace_bytes(const vq_attn_desc* desc, const vq_attn_batch* batch
   st = check_batch_sizes(*desc, batch);
   if (st != VQ_OK) return st;
   if (!bytes) return VQ_ERR_NULL;
-  return attn_workspace(*desc, *batch, bytes);
+  const size_t prompt = prompt_workspace(*desc, *batch), decode = batch->n_tokens == batch->n_seqs ? decode_workspace(*desc, *batch) : 0;
+  *bytes = prompt > decode ? prompt : decode;
+  return VQ_OK;
 }
 
 int vq_attn_decode(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,

@@ -14,43 +14,37 @@ template <bool BF16> __device__ __forceinline__ uint16_t from_f32(float f) {
   else return __builtin_bit_cast(uint16_t, (_Float16)f);
 }
 
-// Work is handed out in tiles of `unit` rows of a sequence (a new token counts `each` rows), at most floor(rows / unit) + extra of
-// them.  Those of sequence i start at slot floor(first row / unit) + extra * i, which leaves room for the last ones of the sequences before;
-// this is the sequence of a slot and the slot's number among its own.  A wave looks at 64 sequences at a time.
-struct Tile { int sequence, number; };
-__device__ __forceinline__ Tile tile_of(const CacheArgs& c, int slot, int each, int unit, int extra) {
-  const int lane = threadIdx.x & 63;
-  int s = 0, start = 0;
-  for (int base = 0; base < c.n_seqs; base += 64) {
-    const int i = base + lane;
-    int at = 0x7fffffff;
-    if (i < c.n_seqs) {
-      int first = c.q_start ? c.q_start[i] : i;
-      first = first < 0 ? 0 : first < c.n_tokens ? first : c.n_tokens;
-      at = first * each / unit + extra * i;
-    }
-    const int before = __popcll(__ballot(at <= slot));
-    if (before == 0) break;   // never in the first turn: sequence 0 starts at slot 0 where q_start is as it should be
-    s = base + before - 1;
-    start = __builtin_amdgcn_readlane(at, before - 1);
-    if (before < 64) break;
-  }
-  return {s, slot - start};
-}
-
 // Tokens in the cache of sequence s: what the table can list at most.
 __device__ __forceinline__ int cached_tokens(const CacheArgs& c, int s) {
   const int n = c.kv_len[s];
   return n < 0 ? 0 : n < c.max_len ? n : c.max_len;
 }
 
-// The rows [*first, *last) of sequence s, inside the arrays whatever q_start holds.
-__device__ __forceinline__ void rows_of(const CacheArgs& c, int s, int* first, int* last) {
-  int a = c.q_start ? c.q_start[s] : s, b = c.q_start ? c.q_start[s + 1] : s + 1;
-  a = a < 0 ? 0 : a < c.n_tokens ? a : c.n_tokens;
-  b = b < a ? a : b < c.n_tokens ? b : c.n_tokens;
-  *first = a;
-  *last = b;
+// Work is handed out in tiles of `unit` rows of a sequence (a new token counts `each` rows), at most floor(rows / unit) + extra of
+// them.  Those of sequence i start at slot floor(first row / unit) + extra * i, which leaves room for the last ones of the sequences before;
+// this is the sequence of a slot, the slot's number among its own, the sequence's rows (new tokens) first .. last - 1 and the tokens
+// in its cache, all inside the arrays whatever they hold.  A wave looks at 64 sequences at a time, with one wait for all of it.
+struct Tile { int sequence, number, first, last, cached; };
+__device__ __forceinline__ Tile tile_of(const CacheArgs& c, int slot, int each, int unit, int extra) {
+  const int lane = threadIdx.x & 63;
+  Tile t = {0, slot, 0, 0, 0};   // an empty sequence, where q_start does not begin with 0
+  for (int base = 0; base < c.n_seqs; base += 64) {
+    const int i = base + lane, in = i < c.n_seqs ? i : c.n_seqs - 1;
+    int first = c.q_start ? c.q_start[in] : in, last = c.q_start ? c.q_start[in + 1] : in + 1;
+    const int cached = cached_tokens(c, in);
+    first = first < 0 ? 0 : first < c.n_tokens ? first : c.n_tokens;
+    last = last < first ? first : last < c.n_tokens ? last : c.n_tokens;
+    const int at = first * each / unit + extra * i;
+    const int before = __popcll(__ballot(i < c.n_seqs && at <= slot));
+    if (before == 0) break;
+    t.sequence = base + before - 1;
+    t.number = slot - __builtin_amdgcn_readlane(at, before - 1);
+    t.first = __builtin_amdgcn_readlane(first, before - 1);
+    t.last = __builtin_amdgcn_readlane(last, before - 1);
+    t.cached = __builtin_amdgcn_readlane(cached, before - 1);
+    if (before < 64) break;
+  }
+  return t;
 }
 
 // A page number from a table, moved into the cache where it lies outside.

@@ -5,7 +5,7 @@ namespace vq {
 namespace {
 
 template <bool BF16>
-hipError_t launch_type(const AttnArgs& a, int head_dim, hipStream_t s) {
+hipError_t launch_type(const PromptArgs& a, int head_dim, hipStream_t s) {
   if (head_dim == 64) return launch_prompt<BF16, 64>(a, s);
   if (head_dim == 96) return launch_prompt<BF16, 96>(a, s);
   return launch_prompt<BF16, 128>(a, s);
@@ -13,7 +13,7 @@ hipError_t launch_type(const AttnArgs& a, int head_dim, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_attn_prompt(const AttnArgs& a, int head_dim, bool bf16, hipStream_t s) {
+hipError_t launch_attn_prompt(const PromptArgs& a, int head_dim, bool bf16, hipStream_t s) {
   if (head_dim == 256) return launch_attn_prompt_256(a, bf16, s);
   return bf16 ? launch_type<true>(a, head_dim, s) : launch_type<false>(a, head_dim, s);
 }

@@ -4,7 +4,7 @@
 
 namespace vq {
 
-hipError_t launch_attn_prompt_256(const AttnArgs& a, bool bf16, hipStream_t s) {
+hipError_t launch_attn_prompt_256(const PromptArgs& a, bool bf16, hipStream_t s) {
   return bf16 ? launch_prompt<true, 256>(a, s) : launch_prompt<false, 256>(a, s);
 }
 

@@ -7,7 +7,7 @@
 namespace vq {
 namespace {
 
-constexpr int kWaves = 4, kRows = kPromptRows, kTokens = 64;   // rows of a workgroup's tile; tokens of a step
+constexpr int kWaves = 4, kRows = kPromptRows, kTokens = kPromptTokens;   // rows of a workgroup's tile; tokens of a step
 static_assert(kRows == 32 * kWaves, "32 rows a wave");
 
 // 16-byte pieces of a row of K in LDS change places so that 16 rows' pieces of one number lie in different banks: piece p of row r
@@ -17,39 +17,73 @@ template <int D> __device__ __forceinline__ int k_turn(int r) {
 }
 
 // One workgroup: 128 rows of one sequence and one key/value head, a row being a (new token, query head of the group) pair, 32 a
-// wave, and all tokens that they attend, 64 at a time.
+// wave, and all tokens that they attend (or a part of them), 64 at a time.
 //   S^T = K Q^T, O^T += V^T P^T, 32 x 32 x 16: a lane has one row's logits (half of a step's), weights and sums, so that a row's
 //   maximum and sum need the other half-wave only, and P goes from the first product's registers into the second's as
 //   it is: row m of the first operand is token m with bits 2 and 3 exchanged, which leaves a lane with eight successive tokens.
 // K and V^T of a step come into LDS past the registers, each wave 16 tokens of both (one page), while the step before is
 // worked on.
 template <bool BF16, int D>
-__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(const PromptArgs A) {
+  const AttnArgs& a = A.a;
   constexpr int KS = D / 16, DT = D / 32, kLoads = D / 32;     // loads of a wave for its 16 tokens' K, and for their V
   constexpr int kHalf = kTokens * D * 2, kStep = 2 * kHalf;    // bytes of K, or V, of a step
   __shared__ __attribute__((aligned(1024))) char lds[2 * kStep];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
   // The heads are neighbours, and so are on the 8 XCDs in turn: those of an XCD keep to their keys and values.  Of the tiles the last come
   // first: they attend most.
-  const int slots = gridDim.x / a.c.kv_heads, kvh = blockIdx.x % a.c.kv_heads, slot = slots - 1 - blockIdx.x / a.c.kv_heads;
-  const int group = a.group;
+  const int group = a.group, heads_in = A.plan.heads, wide = a.heads / heads_in;   // query heads of a tile; tiles beside one another
+  const int slot = (int)A.plan.slots - 1 - blockIdx.x / wide, beside = blockIdx.x % wide, head0 = beside * heads_in, kvh = head0 / group;
+  const Tile tile = tile_of(a.c, slot, heads_in, kRows, 1);
+  const int s = tile.sequence, first = tile.first, n = tile.last - first, len = tile.cached, behind = len - n;   // new token i: position behind + i
+  if (tile.number * kRows >= n * heads_in) return;
+  // The wave's rows: tokens low .. high of its heads (none if low >= n), and the lane's: (token, head), valid or the last one again.
+  int token, head, low, high, most;
+  bool valid;
+  if (A.plan.by_head) {   // 32 tokens of one head
+    const int tokens = kRows / heads_in, at = 32 * wave;
+    low = tile.number * tokens + at % tokens;
+    high = low + 31 < n ? low + 31 : n - 1;
+    most = tile.number * tokens + tokens - 1;
+    token = low + col;
+    head = head0 + at / tokens;
+    valid = token < n;
+  } else {                // all heads of a token after the other
+    const int row = tile.number * kRows + 32 * wave, end = n * heads_in - 1;
+    low = row / heads_in;
+    high = (row + 31 < end ? row + 31 : end) / heads_in;
+    most = (tile.number * kRows + kRows - 1) / heads_in;
+    valid = row + col <= end;
+    const int mine = valid ? row + col : end;
+    token = mine / heads_in;
+    head = head0 + mine - token * heads_in;
+    low = row <= end ? low : n;
+  }
+  token = token < n ? token : n - 1;
+  most = behind + (most < n ? most : n - 1);
+  const int pos = behind + token, wave_first = behind + low, wave_last = low < n ? behind + high : -1;
+  const int all = most < 0 ? 0 : most / kTokens + 1;       // steps of the tile, and this part's: begin .. steps - 1
+  const int begin = blockIdx.y * A.plan.steps, steps = all - begin < A.plan.steps ? all : begin + A.plan.steps;
+  if (begin >= all && begin > 0) return;
 
-  const Tile tile = tile_of(a.c, slot, group, kRows, 1);
-  const int s = tile.sequence;
-  int first, last;
-  rows_of(a.c, s, &first, &last);
-  const int n = last - first, rows = n * group, row0 = tile.number * kRows;
-  if (row0 >= rows) return;
-  const int len = cached_tokens(a.c, s), behind = len - n;   // new token i has position behind + i
-  const int row = row0 + 32 * wave + col, row_in = row < rows ? row : rows - 1;
-  const int token = row_in / group, head = kvh * group + (row_in - token * group);
-  const int pos = behind + token;
-  const int wave_row = row0 + 32 * wave;
-  const int wave_last = wave_row < rows ? behind + ((wave_row + 31 < rows ? wave_row + 31 : rows - 1) / group) : -1;   // highest position
-  const int wave_first = behind + wave_row / group;
-  const int most = behind + ((row0 + kRows - 1 < rows ? row0 + kRows - 1 : rows - 1) / group);
-  const int steps = most < 0 ? 0 : most / kTokens + 1;
-
+  // Loads: the wave's tokens are 16 wave .. + 15 of the step.  K: rows of D values, their pieces turned; V^T: for each dimension two
+  // pieces of eight tokens, exchanged where bit 3 of the dimension is set.
+  const int shift = a.c.page_shift, mask = (1 << shift) - 1, last_page = len > 0 ? (len - 1) >> shift : 0;
+  uint32_t k_off[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int at = 64 * j + lane, r = at / (D / 8), p = at % (D / 8);
+    k_off[j] = (r * D + (p ^ k_turn<D>(r)) * 8) * 2;
+  }
+  const uint32_t v_off = (((lane >> 1) << shift) + 8 * ((lane & 1) ^ ((lane >> 4) & 1))) * 2;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
+  const int32_t* table = a.c.table + (int64_t)s * a.c.table_width;
+  // Lane i: the wave's page in step begin + i (mod 64) of the 64 that are being loaded; asked for before q, which the loads need not wait for.
+  auto pages_from = [&](int step) {
+    const int j = ((step + lane) * kTokens + 16 * wave) >> shift;
+    return table[j < last_page ? j : last_page];
+  };
+  int pages = pages_from(begin);
   u32x4 q[KS];
   {
     const uint16_t* from = a.q + (int64_t)(first + token) * a.qs.token + head * a.qs.head;
@@ -67,28 +101,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
     }
   }
 
-#pragma unroll
-  for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));   // here, or the compiler waits for them in the loop, and with them for its loads
-
-  // Loads: the wave's tokens are 16 wave .. + 15 of the step.  K: rows of D values, their pieces turned; V^T: for each dimension two
-  // pieces of eight tokens, exchanged where bit 3 of the dimension is set.
-  const int shift = a.c.page_shift, mask = (1 << shift) - 1, last_page = len > 0 ? (len - 1) >> shift : 0;
-  uint32_t k_off[kLoads];
-#pragma unroll
-  for (int j = 0; j < kLoads; ++j) {
-    const int at = 64 * j + lane, r = at / (D / 8), p = at % (D / 8);
-    k_off[j] = (r * D + (p ^ k_turn<D>(r)) * 8) * 2;
-  }
-  const uint32_t v_off = (((lane >> 1) << shift) + 8 * ((lane & 1) ^ ((lane >> 4) & 1))) * 2;
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
-  const int32_t* table = a.c.table + (int64_t)s * a.c.table_width;
-  int pages = 0;   // lane i: the wave's page in step i (mod 64) of the 64 that are being loaded
   auto load = [&](int step) {
-    if ((step & 63) == 0) {
-      const int j = ((step + lane) * kTokens + 16 * wave) >> shift;
-      pages = table[j < last_page ? j : last_page];
-    }
-    const int page = page_inside(a.c, __builtin_amdgcn_readlane(pages, step & 63));
+    const int at = (step - begin) & 63;
+    if (at == 0 && step > begin) pages = pages_from(step);
+    const int page = page_inside(a.c, __builtin_amdgcn_readlane(pages, at));
     const int in = (step * kTokens + 16 * wave) & mask;
     const int64_t page_head = ((int64_t)page * a.c.kv_heads + kvh) * ((int64_t)D << shift);
     const uint16_t* k = a.k_pages + page_head + in * D;
@@ -99,6 +115,11 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) load_to_lds(v + ((int64_t)(32 * j) << shift), v_off, to + kHalf + 1024 * j);
   };
+
+  int step = begin;
+  if (step < steps) load(step);
+#pragma unroll
+  for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));   // here, or the compiler waits for them in the loop, and with them for its loads
 
   float m = -INFINITY, from = 0.f, l = 0.f;   // as in the kernel of one new token
   f32x16 o[DT];
@@ -113,32 +134,32 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
     const char* kt = lds + (step & 1) * kStep;
     const char* vt = kt + kHalf;
     f32x16 x[2];
-    u32x4 f[4 * DT];   // an operand's fragments, all asked for before the first is used (KS = 2 DT)
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int r = 32 * t + k_row;
-        f[2 * k + t] = *reinterpret_cast<const u32x4*>(kt + (r * (D / 8) + ((2 * k + half) ^ k_turn<D>(r))) * 16);
-      }
-    __builtin_amdgcn_sched_barrier(0);
+    // An operand's fragments, up to 16 asked for before the first is used.  (KS = 2 DT: both products have 4 DT.)
+    constexpr int kBatch = 4 * DT < 16 ? 4 * DT : 16;
+    u32x4 f[kBatch];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int j = 0; j < 16; ++j) x[t][j] = 0.f;
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
+    for (int k0 = 0; k0 < KS; k0 += kBatch / 2) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) x[t] = mfma32<BF16>(f[2 * k + t], q[k], x[t]);
-    __builtin_amdgcn_sched_barrier(0);
-    const char* v_at = vt + col * 32 + (half ^ ((col >> 3) & 1)) * 16;
-    if constexpr (!masked) {
+      for (int k = 0; k < kBatch; ++k) {
+        const int r = 32 * (k & 1) + k_row;
+        f[k] = *reinterpret_cast<const u32x4*>(kt + (r * (D / 8) + ((2 * (k0 + k / 2) + half) ^ k_turn<D>(r))) * 16);
+      }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int i = 0; i < DT; ++i) f[c * DT + i] = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32);
+      for (int k = 0; k < kBatch; ++k) x[k & 1] = mfma32<BF16>(f[k], q[k0 + k / 2], x[k & 1]);
       __builtin_amdgcn_sched_barrier(0);
     }
+    const char* v_at = vt + col * 32 + (half ^ ((col >> 3) & 1)) * 16;
+    auto v_batch = [&](int at) {   // fragments at .. of V^T: 32 dimensions of the first 16 tokens, the next 32, ..
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) f[j] = *reinterpret_cast<const u32x4*>(v_at + ((at + j) / DT * D + (at + j) % DT * 32) * 32);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    if constexpr (!masked) v_batch(0);   // under way while the weights are made
     const int rel = pos - step * kTokens - 8 * half;   // tokens of the lane up to here are attended
     if constexpr (masked) {
 #pragma unroll
@@ -210,17 +231,17 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
       }
     } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int at = 0; at < 4 * DT; at += kBatch) {
+        if (at > 0) v_batch(at);
 #pragma unroll
-        for (int i = 0; i < DT; ++i) o[i] = mfma32<BF16>(f[c * DT + i], p[c], o[i]);
+        for (int j = 0; j < kBatch; ++j) o[(at + j) % DT] = mfma32<BF16>(f[j], p[(at + j) / DT], o[(at + j) % DT]);
+      }
     }
   };
 
   // First the steps whose tokens all of the wave's rows attend.
-  const int whole = wave_row < rows && wave_first >= 0 ? (wave_first + 1) / kTokens : 0;
-  if (steps > 0) load(0);
-  int step = 0;
-  for (; step < whole; ++step) {
+  const int whole = low < n && wave_first >= 0 ? (wave_first + 1) / kTokens : 0;
+  for (; step < whole && step < steps; ++step) {
     lds_turn();
     if (step + 1 < steps) load(step + 1);
     work(step, std::false_type());
@@ -232,25 +253,89 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
   }
 
   l += __shfl_xor(l, 32);
-  if (wave_row >= rows) return;
+  const int parts = (all + A.plan.steps - 1) / A.plan.steps;
+  if (parts > 1) {
+    // Whoever finishes last joins the parts, in their order.  A lane's numbers lie where the same lane finds them: [part][maximum and sum
+    // of the weights, then two sums over values at a time][lane].
+    __shared__ uint32_t arrived;
+    constexpr int kPairs = 1 + 8 * DT;
+    const int64_t unit = (int64_t)slot * wide + beside;
+    float* mine = A.part + ((unit * A.plan.parts * kWaves + wave) * kPairs * 64 + lane) * 2;   // of part 0
+    constexpr int64_t kPart = (int64_t)kWaves * kPairs * 128;
+    if (low < n) {
+      float* to = mine + blockIdx.y * kPart;
+      shared_store(to, m, l);
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) shared_store(to + (1 + 8 * i + j) * 128, o[i][2 * j], o[i][2 * j + 1]);
+    }
+    shared_stores_done();
+    __syncthreads();
+    if (tid == 0) arrived = __hip_atomic_fetch_add(&A.counter[unit], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (arrived != (uint32_t)parts - 1) return;
+    if (tid == 0) __hip_atomic_store(&A.counter[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (low >= n) return;
+    m = -INFINITY;
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, shared_load(mine + p * kPart)[0]);
+    const float base = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    for (int p = 0; p < parts; ++p) {
+      const float* of = mine + p * kPart;
+      const f32x2 ml = shared_load(of);
+      const float f = exp2_fast(ml[0] - base);
+      l += f * ml[1];
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const f32x2 v = shared_load(of + (1 + 8 * i + j) * 128);
+          o[i][2 * j] += f * v[0];
+          o[i][2 * j + 1] += f * v[1];
+        }
+    }
+  }
   const bool any = pos >= 0;
   const float scale = any ? 1.f / l : 0.f;
-  if (row >= rows) return;
   uint16_t* to = a.out + (int64_t)(first + token) * a.os.token + head * a.os.head;
+  if (a.os.dim == 1 && ((a.os.token | a.os.head) & 7) == 0) {
+    // The half-waves exchange fours of dimensions, which leaves a lane with eight in a row.
 #pragma unroll
-  for (int i = 0; i < DT; ++i)
+    for (int i = 0; i < DT; ++i)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const int64_t d = 32 * i + 8 * (j >> 2) + 4 * half + (j & 3);
-      to[d * a.os.dim] = from_f32<BF16>(any ? o[i][j] * scale : 0.f);
-    }
-  if (a.lse && half == 0) a.lse[(int64_t)(first + token) * a.heads + head] = any ? (m + __log2f(l)) * 0.693147180559945f : -INFINITY;
+      for (int b = 0; b < 2; ++b) {
+        f32x8 v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = any ? o[i][8 * b + j] * scale : 0.f;
+        u32x4 w = pack8<BF16>(v);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const auto r = __builtin_amdgcn_permlane32_swap(w[j], w[2 + j], false, false);
+          w[j] = r[0];
+          w[2 + j] = r[1];
+        }
+        if (valid) *reinterpret_cast<u32x4*>(to + 32 * i + 16 * b + 8 * half) = w;
+      }
+  } else if (valid) {
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int64_t d = 32 * i + 8 * (j >> 2) + 4 * half + (j & 3);
+        to[d * a.os.dim] = from_f32<BF16>(any ? o[i][j] * scale : 0.f);
+      }
+  }
+  if (a.lse && half == 0 && valid) a.lse[(int64_t)(first + token) * a.heads + head] = any ? (m + __log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
 template <bool BF16, int D>
-hipError_t launch_prompt(const AttnArgs& a, hipStream_t s) {
-  const int64_t slots = (int64_t)a.c.n_tokens * a.group / kPromptRows + a.c.n_seqs;
-  prompt_kernel<BF16, D><<<(unsigned)(a.c.kv_heads * slots), 64 * kWaves, 0, s>>>(a);
+hipError_t launch_prompt(const PromptArgs& a, hipStream_t s) {
+  prompt_kernel<BF16, D><<<dim3((unsigned)(a.a.heads / a.plan.heads * a.plan.slots), a.plan.parts), 64 * kWaves, 0, s>>>(a);
   return hipGetLastError();
 }
 

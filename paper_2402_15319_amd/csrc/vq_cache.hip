@@ -28,11 +28,9 @@ __device__ __forceinline__ int64_t head_of(const CacheArgs& c, int s, int pos, i
 // A token at a time: a thread takes eight dimensions of a head's key and value.
 __global__ __launch_bounds__(256) void append_one_kernel(const AppendArgs a, int head_dim) {
   const int t = blockIdx.x, pieces = head_dim / 8, i = blockIdx.y * 256 + threadIdx.x, h = i / pieces, d = 8 * (i - h * pieces);
-  const int s = a.c.q_start ? tile_of(a.c, t, 1, 1, 0).sequence : t;
-  int first, last;
-  rows_of(a.c, s, &first, &last);
-  const int pos = cached_tokens(a.c, s) - last + t;
-  if (h >= a.c.kv_heads || t < first || t >= last || pos < 0) return;
+  const Tile tile = a.c.q_start ? tile_of(a.c, t, 1, 1, 0) : Tile{t, 0, t, t + 1, cached_tokens(a.c, t)};
+  const int s = tile.sequence, pos = tile.cached - tile.last + t;
+  if (h >= a.c.kv_heads || t < tile.first || t >= tile.last || pos < 0) return;
   const int size = 1 << a.c.page_shift, slot = pos & (size - 1);
   const uint16_t* k = a.k + t * a.ks.token + h * a.ks.head + d * a.ks.dim;
   const uint16_t* v = a.v + t * a.vs.token + h * a.vs.head + d * a.vs.dim;
@@ -63,10 +61,8 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const App
   const bool values = wave >= kHalves;
   const int h = blockIdx.x % a.c.kv_heads;
   const Tile tile = tile_of(a.c, blockIdx.x / a.c.kv_heads, 1, kTile, 2);
-  const int s = tile.sequence;
-  int first, last;
-  rows_of(a.c, s, &first, &last);
-  const int behind = cached_tokens(a.c, s) - last, from = behind + first > 0 ? behind + first : 0;   // token t has position behind + t
+  const int s = tile.sequence, first = tile.first, last = tile.last;
+  const int behind = tile.cached - last, from = behind + first > 0 ? behind + first : 0;   // token t has position behind + t
   // lanes: positions first where the source runs along them, dimensions first where it runs along those
   const Strides st = values ? a.vs : a.ks;
   const bool along_tokens = st.token == 1 && st.dim != 1;

@@ -72,10 +72,23 @@ hipError_t launch_attn_decode(const DecodeArgs& d, int head_dim, bool, hipStream
   return hipSuccess;
 }
 
-hipError_t launch_attn_prompt(const AttnArgs& a, int head_dim, bool, hipStream_t) {
+hipError_t launch_attn_prompt(const PromptArgs& d, int head_dim, bool, hipStream_t) {
+  const AttnArgs& a = d.a;
+  const PromptPlan& p = d.plan;
   check_attn(a, head_dim);
+  // a slot for every tile, every step in a part, no part that the longest sequence leaves empty
+  REQUIRE(p.heads >= 1 && a.group % p.heads == 0 && (p.by_head ? p.heads == 1 || p.heads == 2 || p.heads == 4 : p.heads == a.group));
+  REQUIRE(p.slots == (long long)a.c.n_tokens * p.heads / kPromptRows + a.c.n_seqs);
+  const long long wide = a.heads / p.heads;
+  REQUIRE(p.slots * wide * 256 < 4294967296ll);
+  REQUIRE(p.steps >= 1 && p.parts >= 1 && p.parts <= 65535 && (long long)p.steps * p.parts * kPromptTokens >= a.c.max_len);
+  REQUIRE(p.parts == 1 || (long long)p.steps * (p.parts - 1) * kPromptTokens < a.c.max_len);
+  if (p.parts > 1) {
+    REQUIRE(p.slots * wide <= kJoinCounters);
+    const size_t end = (size_t)((char*)d.part - (char*)d.counter) + (size_t)p.slots * wide * p.parts * prompt_part_floats(head_dim) * 4;
+    REQUIRE((char*)d.part - (char*)d.counter >= kJoinCounters * 4 && end <= g_workspace);
+  }
   REQUIRE((long long)a.c.n_tokens * a.group + kPromptRows < 2147483647);   // rows of a key/value head
-  REQUIRE(((long long)a.c.n_tokens * a.group / kPromptRows + a.c.n_seqs) * a.c.kv_heads * 256 < 4294967296ll);
   return hipSuccess;
 }
 }  // namespace vq
@@ -134,7 +147,7 @@ static void calls(std::mt19937& rng) {
     b.page_table = (const int32_t*)at(2);
     b.q_start = one_each ? nullptr : (const int32_t*)at(3);
     size_t n = 0;
-    if ((long long)b.n_tokens * d.heads / 128 + (long long)b.n_seqs * d.kv_heads > 1 << 20) {
+    if ((long long)b.n_tokens * d.heads / 128 + (long long)b.n_seqs * d.heads > 1 << 20) {
       REQUIRE(vq_attn_workspace_bytes(&d, &b, &n) == VQ_ERR_BAD_ARG);
       continue;
     }
@@ -147,7 +160,9 @@ static void calls(std::mt19937& rng) {
     const long long before = vq::g_launches;
     REQUIRE(vq_attn_prompt(&d, &b, at(4), s, at(5), at(6), at(7), s, rng() % 2 ? (float*)at(8) : nullptr, at(9), n, nullptr) == VQ_OK);
     if (one_each) REQUIRE(vq_attn_decode(&d, &b, at(4), s, at(5), at(6), at(7), s, nullptr, at(9), n, nullptr) == VQ_OK);
-    REQUIRE(vq_attn_prompt(&d, &b, at(4), s, at(5), at(6), at(7), s, nullptr, at(9), n - 1, nullptr) == VQ_ERR_BAD_ARG);
+    const bool short_prompt = vq_attn_prompt(&d, &b, at(4), s, at(5), at(6), at(7), s, nullptr, at(9), n - 1, nullptr) == VQ_ERR_BAD_ARG;
+    const bool short_decode = b.n_tokens == b.n_seqs && vq_attn_decode(&d, &b, at(4), s, at(5), at(6), at(7), s, nullptr, at(9), n - 1, nullptr) == VQ_ERR_BAD_ARG;
+    REQUIRE(short_prompt || short_decode);   // no more than one of them needs
     REQUIRE(vq_cache_append(&d, &b, at(4), nullptr, at(5), nullptr, at(6), at(7), nullptr) == VQ_OK);
     REQUIRE(vq::g_launches > before);
   }
