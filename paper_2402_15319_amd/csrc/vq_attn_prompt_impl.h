@@ -134,6 +134,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
     const char* kt = lds + (step & 1) * kStep;
     const char* vt = kt + kHalf;
     f32x16 x[2];
+    // The products of the logits go before another wave's weights (nine packed prompts 94 to 95 us, 98 without).
+    __builtin_amdgcn_s_setprio(1);
     // An operand's fragments, up to 16 asked for before the first is used.  (KS = 2 DT: both products have 4 DT.)
     constexpr int kBatch = 4 * DT < 16 ? 4 * DT : 16;
     u32x4 f[kBatch];
@@ -160,6 +162,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
       __builtin_amdgcn_sched_barrier(0);
     };
     if constexpr (!masked) v_batch(0);   // under way while the weights are made
+    __builtin_amdgcn_s_setprio(0);
     const int rel = pos - step * kTokens - 8 * half;   // tokens of the lane up to here are attended
     if constexpr (masked) {
 #pragma unroll
