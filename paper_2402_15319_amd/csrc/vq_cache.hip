@@ -67,7 +67,11 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const App
   const Strides st = values ? a.vs : a.ks;
   const bool along_tokens = st.token == 1 && st.dim != 1;
   const int x = along_tokens ? lane & 7 : lane >> 3, y = along_tokens ? lane >> 3 : lane & 7;
-  const int pos = (from / kTile + tile.number) * kTile + 8 * x, d = 64 * (wave % kHalves) + 8 * y;
+  const int pos = (from / kTile + tile.number) * kTile + 8 * x;
+  // Its dimensions: 8 y .. + 7, or, where nothing is turned, every eighth from y, so that the lanes of an instruction have successive ones.
+  const bool spread = D % 64 == 0 && values && along_tokens;
+  const int d = 64 * (wave % kHalves) + (spread ? y : 8 * y), d_step = spread ? 8 : 1;
+  const int64_t dim = st.dim * d_step;
   const int lo = from - pos > 0 ? from - pos : 0, end = behind + last - pos, hi = end < 8 ? end : 8;   // its positions lo .. hi - 1 are new
   if (lo >= hi || d >= D) return;
   const int64_t base = head_of(a.c, s, pos, h, D);
@@ -82,13 +86,13 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const App
   } else if (st.token == 1 && whole) {
     by_token = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) in[i] = *reinterpret_cast<const u32x4_any*>(src + i * st.dim);
+    for (int i = 0; i < 8; ++i) in[i] = *reinterpret_cast<const u32x4_any*>(src + i * dim);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint16_t* row = src + (i < lo ? lo : i < hi ? i : hi - 1) * st.token;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) in[i][j] = row[2 * j * st.dim] | (uint32_t)row[(2 * j + 1) * st.dim] << 16;
+      for (int j = 0; j < 4; ++j) in[i][j] = row[2 * j * dim] | (uint32_t)row[(2 * j + 1) * dim] << 16;
     }
   }
   if (by_token == values) {
@@ -106,13 +110,13 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const App
     uint16_t* to = a.v_pages + base + (int64_t)d * size + slot;
     if (whole) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(to + i * size) = in[i];
+      for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(to + i * d_step * size) = in[i];
     } else {   // other tokens' slots stay as they are
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (j >= lo && j < hi) to[i * size + j] = (uint16_t)(in[i][j / 2] >> (j % 2 * 16));
+          if (j >= lo && j < hi) to[i * d_step * size + j] = (uint16_t)(in[i][j / 2] >> (j % 2 * 16));
     }
   }
 }
