@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256) void append_one_kernel(const AppendArgs a, int
 // Any number of new tokens: a workgroup takes 64 positions of a sequence and a head, half of its waves the keys and half the
 // values, a lane eight positions by eight dimensions in registers.  Loads and stores are 16 bytes along whatever is contiguous, 128
 // in a row of lanes; where the source runs along the other index than the page, the lane turns its block.
-constexpr int kTile = 64, kFewTokens = 8;
+constexpr int kTile = 64;
 template <int D>
 __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const AppendArgs a) {
   constexpr int kHalves = (D + 63) / 64;
@@ -142,9 +142,10 @@ __global__ __launch_bounds__(256) void copy_kernel(const CopyArgsOf<PAIRS> a) {
 }  // namespace
 
 hipError_t launch_append(const AppendArgs& a, int head_dim, hipStream_t s) {
-  // Few new tokens for each sequence: blocks of eight positions would be mostly empty (64 sequences with one each, 32 heads: %s us, %s
-  // in blocks; %s).
-  if (!a.c.q_start || a.c.n_tokens <= kFewTokens * (int64_t)a.c.n_seqs) {
+  // Few new tokens for each sequence: most of a block of eight positions would be empty (64 sequences x 32 heads of 128, in the order of the
+  // batched product: one new token each 7.6 us, 15.7 in blocks; two 11.9 and 16.2; four 19.5 and 17.5).  Few altogether: a block's
+  // turn takes longer than they do (16 tokens of 8 sequences x 8 heads 5.0 and 8.5 us; 32 of one x 32 heads 5.8 and 6.0).
+  if (!a.c.q_start || a.c.n_tokens <= 2 * (int64_t)a.c.n_seqs || (int64_t)a.c.n_tokens * a.c.kv_heads <= 1024) {
     append_one_kernel<<<dim3(a.c.n_tokens, (a.c.kv_heads * head_dim / 8 + 255) / 256), 256, 0, s>>>(a, head_dim);
     return hipGetLastError();
   }

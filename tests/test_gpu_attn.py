@@ -204,3 +204,63 @@ def test_offsets_beyond_32_bits():
     small.check(*run(small, "decode"))
     small.check(*run(small, "prompt"))
     assert torch_type("f16") == torch.float16
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads, kv", [(4, 4), (4, 2), (8, 2), (7, 1), (12, 1)])
+@pytest.mark.parametrize("layout, gap", [("tokens", 1), ("heads", 0), ("features", 0), ("odd", 0), ("odd features", 0)])
+def test_long_prompts_in_every_order(layout, gap, heads, kv, dtype):
+    """Prompts long enough that a wave takes successive tokens of one head, some of them with an end inside a wave, some empty."""
+    p = Problem(heads, kv, 64, 32, dtype, [290, 0, 410, 33, 127], [257, 0, 128, 33, 127], layout=layout, gap=gap, seed=heads)
+    p.check(*run(p))
+
+
+@pytest.mark.parametrize("dim, page", [(96, 16), (128, 64), (256, 32), (256, 128)])
+def test_long_prompts_of_every_size_of_head(dim, page):
+    p = Problem(4, 1, dim, page, "f16", [400, 333], [300, 333], seed=dim)
+    p.check(*run(p))
+
+
+@pytest.mark.parametrize("call", ["decode", "prompt"])
+def test_many_sequences(call):
+    """More than a wave looks at in one turn, with none, one or a few tokens."""
+    rng = np.random.default_rng(1)
+    lens = rng.integers(0, 40, 200).tolist()
+    new = None if call == "decode" else [int(rng.integers(0, n + 1)) for n in lens]
+    p = Problem(4, 2, 64, 16, "bf16", lens, new, seed=2)
+    p.check(*run(p, call))
+
+
+@pytest.mark.parametrize("call", ["decode", "prompt"])
+def test_nothing_in_any_cache(call):
+    import torch
+    p = Problem(4, 2, 64, 16, "f16", [0, 0, 0], [1, 1, 1], seed=2)
+    out, lse = run(p, call, max_len=0)
+    assert not out.any() and bool(torch.isneginf(lse).all())
+
+
+@pytest.mark.parametrize("new", [1, 5, 40])
+def test_prompts_of_few_rows_behind_many_tokens(new):
+    """Split over the length and joined, with every layout of heads that a tile can have."""
+    for heads, kv in ((4, 4), (6, 2), (4, 1), (20, 1)):
+        p = Problem(heads, kv, 64, 16, "f16", [3000, 2500 - new, 70], [new, 2, 0], seed=heads)
+        p.check(*run(p))
+
+
+def test_a_prompt_is_what_its_tokens_are_one_at_a_time():
+    """Every row of a prompt against the call for one new token with that many tokens in the cache: two roundings apart."""
+    import torch
+    import paper_2402_15319_amd as vq
+    p = Problem(4, 2, 128, 16, "f16", [200], [200], seed=4)
+    out, lse = run(p)
+    ref = p.reference()
+    b_out, b_lse = p.bounds(ref)
+    got = torch.empty_like(out)
+    got_lse = torch.empty_like(lse)
+    for t in range(200):
+        lens = torch.tensor([t + 1], dtype=torch.int32, device="cuda:0")
+        batch = vq.AttnBatch(lens, p.table_d, max_len=t + 1)
+        vq.vq_attn_decode(p.desc, batch, p.q[t:t + 1], p.k_pages, p.v_pages, got[t:t + 1], vq.attn_workspace(p.desc, batch), lse=got_lse[t:t + 1])
+    torch.cuda.synchronize()
+    assert (np.abs((got - out).double().cpu().numpy()) <= 2 * b_out).all()
+    assert (np.abs((got_lse - lse).double().cpu().numpy()) <= 2 * b_lse).all()

@@ -108,3 +108,89 @@ def test_pages_are_copied_one_pair_after_another(n_buffers, pages, kv, dim, page
     vq.vq_cache_copy(desc, list(caches.unbind(0)), pairs)
     torch.cuda.synchronize()
     np.testing.assert_array_equal(caches.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("layout", ["tokens", "features"])
+@pytest.mark.parametrize("new", [1, 2, 3, 20])
+def test_many_sequences(new, layout):
+    """More than a wave looks at in one turn; few new tokens for each and more, some sequences without any."""
+    import torch
+    rng = np.random.default_rng(new)
+    news = [0 if rng.random() < 0.1 else new for _ in range(150)]
+    news[0] = new
+    lens = [n + int(rng.integers(0, 30)) for n in news]
+    p = Problem(8, 8, 64, 16, "f16", lens, news, layout=layout, seed=new)
+    gen = torch.Generator().manual_seed(7)
+    k_host = torch.randint(-32768, 32768, (p.total, 8, 64), generator=gen, dtype=torch.int32).to(torch.int16)
+    k = p.rows(k_host.view(torch.float16), 8)
+    kp, vp = _append(p, k, k)
+    want = ao.append(k_host.numpy(), k_host.numpy(), _bits(p.k_pages), _bits(p.v_pages), p.table, p.lens, p.q_start)
+    np.testing.assert_array_equal(_bits(kp), want[0])
+    np.testing.assert_array_equal(_bits(vp), want[1])
+
+
+def test_more_new_tokens_than_the_cache_counts():
+    """The first of them have negative positions and are left out."""
+    import torch
+    p = Problem(2, 2, 96, 16, "f16", [70, 3, 0], [100, 40, 9], layout="features", seed=1)
+    k_host = torch.randn(p.total, 2, 96).half()
+    k = p.rows(k_host, 2)
+    kp, vp = _append(p, k, k)
+    want = ao.append(_bits(k_host), _bits(k_host), _bits(p.k_pages), _bits(p.v_pages), p.table, p.lens, p.q_start)
+    np.testing.assert_array_equal(_bits(kp), want[0])
+    np.testing.assert_array_equal(_bits(vp), want[1])
+
+
+def test_offsets_beyond_32_bits():
+    """Pages at the end of buffers of more than 2^32 bytes, as a place for tokens and as a copy's source and target."""
+    import torch
+    import paper_2402_15319_amd as vq
+    pages = 2 ** 32 // (2 * 128 * 128 * 2) + 70
+    k = torch.zeros(pages, 2, 128, 128, dtype=torch.float16, device="cuda:0")
+    v = torch.zeros(pages, 2, 128, 128, dtype=torch.float16, device="cuda:0")
+    desc = vq.make_attn_desc(2, 2, 128, 128, pages)
+    table = torch.tensor([[pages - 1, pages - 5]], dtype=torch.int32, device="cuda:0")
+    lens = torch.tensor([200], dtype=torch.int32, device="cuda:0")
+    start = torch.tensor([0, 200], dtype=torch.int32, device="cuda:0")
+    batch = vq.AttnBatch(lens, table, n_tokens=200, max_len=200, q_start=start)
+    rows = torch.randn(200, 2, 128, device="cuda:0").half()
+    vq.vq_cache_append(desc, batch, rows, rows, k, v)
+    vq.vq_cache_copy(desc, [k, v], [(pages - 1, 3), (pages - 5, pages - 2)])
+    torch.cuda.synchronize()
+    for first, second in ((pages - 1, pages - 5), (3, pages - 2)):
+        assert torch.equal(torch.cat([k[first].transpose(0, 1), k[second].transpose(0, 1)])[:200], rows)
+        assert torch.equal(torch.cat([v[first].permute(2, 0, 1), v[second].permute(2, 0, 1)])[:200], rows)
+    assert int(k.count_nonzero()) <= 2 * rows.numel() and not k[4:pages - 10].any()
+
+
+def test_append_and_copy_in_a_captured_graph_and_on_another_stream():
+    """A graph follows the lengths and the table when it is replayed."""
+    import torch
+    import paper_2402_15319_amd as vq
+    p = Problem(4, 4, 64, 16, "f16", [40, 17], [1, 1], seed=3)
+    rows = torch.randn(2, 4, 64, device="cuda:0").half()
+    kp, vp = p.k_pages.clone(), p.v_pages.clone()
+    batch = vq.AttnBatch(p.lens_d, p.table_d, max_len=p.width * 16)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        vq.vq_cache_append(p.desc, batch, rows, rows, kp, vp)
+        vq.vq_cache_copy(p.desc, [kp], [(0, 1)])
+    for lens in ([40, 17], [33, 2], [38, 16]):
+        p.lens_d.copy_(torch.tensor(lens, dtype=torch.int32))
+        kp.copy_(p.k_pages)
+        vp.copy_(p.v_pages)
+        rows.normal_()
+        g.replay()
+        torch.cuda.synchronize()
+        want = ao.append(_bits(rows), _bits(rows), _bits(p.k_pages), _bits(p.v_pages), p.table, lens, p.q_start)
+        np.testing.assert_array_equal(_bits(kp), ao.copy_pages(want[0][None], [(0, 1)])[0])
+        np.testing.assert_array_equal(_bits(vp), want[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    kp.copy_(p.k_pages)
+    side.wait_stream(torch.cuda.current_stream())
+    vq.vq_cache_append(p.desc, batch, rows, rows, kp, vp, stream=side)
+    vq.vq_cache_copy(p.desc, [kp], [(0, 1)], stream=side)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(_bits(kp), ao.copy_pages(want[0][None], [(0, 1)])[0])
