@@ -47,10 +47,11 @@ struct AttnArgs {
 struct DecodePlan {
   int32_t chunk, parts;   // tokens of a part; parts of the longest sequence
   int32_t tiles, cols;    // tiles of a key/value head's query heads; query heads of a tile at most
+  int32_t together;       // tiles of a workgroup: 1, 2 or 3
   int32_t waves;          // of a workgroup: 4 or 8; each takes 32 tokens in turn
 };
 constexpr int kJoinCounters = 16384;   // at the start of the workspace: parts that have finished, zero between calls
-constexpr int kTileHeads = 16;
+constexpr int kTileHeads = 16, kTogetherDim = 128;   // several tiles up to this head_dim: the sums of larger ones leave no registers for it
 constexpr int kMostParts = 64;         // of a sequence
 
 struct DecodeArgs {

@@ -89,6 +89,7 @@ int check_strides(const vq_strides* in, int n_tokens, int heads, int head_dim, b
 
 constexpr int kPartStep = 128;            // tokens that a workgroup takes at a time
 constexpr int64_t kEnoughUnits = 256;     // workgroups: one for each CU
+constexpr int64_t kTogetherUnits = 16;
 constexpr int kLongPart = 4096, kShortPart = 1024;
 constexpr int kShortValues = 32768;       // of a sequence's keys: no parts up to here
 
@@ -97,15 +98,19 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   const int group = d.heads / d.kv_heads;
   p.tiles = (group + kTileHeads - 1) / kTileHeads;
   p.cols = group < kTileHeads ? group : kTileHeads;
-  const int64_t units = (int64_t)b.n_seqs * d.kv_heads * p.tiles;
+  p.together = d.head_dim > kTogetherDim || p.tiles == 1 ? 1 : p.tiles == 2 || p.tiles == 4 ? 2 : 3;
+  // Three tiles together read a key/value head once, but leave one workgroup to join all of their parts: with 48 heads to one of 128 and
+  // sequences of up to 8,192, 64 of them take 63 us (a tile to a workgroup 115), 32 42 (74), 16 46 (43) and 8 50 (29).
+  if ((int64_t)b.n_seqs * d.kv_heads * ((p.tiles + p.together - 1) / p.together) < kTogetherUnits) p.together = 1;
+  const int64_t units = (int64_t)b.n_seqs * d.kv_heads * ((p.tiles + p.together - 1) / p.together);
   const int64_t steps = b.max_len > kPartStep ? ((int64_t)b.max_len + kPartStep - 1) / kPartStep : 1;
   int64_t parts = 1;
   p.waves = 4;
   if ((int64_t)b.max_len * d.head_dim <= kShortValues) {
     // One part of 8 waves: a step or two for each of them cost less than the join (a sequence of 256 tokens x 32 heads of 128 6.1
     // us, in two parts of 4 waves 7.7; of 512 8.9 and 8.0; of 512 x 32 heads of 64 5.6 and 7.7).
-    p.waves = b.max_len > 32 * p.waves ? 8 : 4;
-  } else if (units <= kJoinCounters) {
+    p.waves = b.max_len > 32 * p.waves && p.together == 1 ? 8 : 4;
+  } else if (units * p.together <= kJoinCounters) {
     // A workgroup for every CU is enough where they are of one size (130,001 tokens x 8 heads: 256 workgroups 97 us, 512 100,
     // 1,024 106).  Where there are as many without a split, the lengths will differ, and parts of 1,024 tokens even them
     // out (61 sequences of 1 to 8,192: parts of 1,024 68 us, of 2,048 77, of 4,096 85; 24 of 2,048 to 4,096 alike: 203 and 202).

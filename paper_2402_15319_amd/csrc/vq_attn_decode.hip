@@ -4,7 +4,7 @@
 namespace vq {
 namespace {
 
-// One workgroup: `chunk` tokens of a sequence, the query heads (up to 16) of a tile.  Its waves take 32 tokens at a time in turn.
+// One workgroup: `chunk` tokens of a sequence, the query heads of TILES tiles of up to 16.  Its waves take 32 tokens at a time in turn.
 //   S^T = K Q^T: two instructions' rows are 16 tokens each, their columns the query heads.  The rows' tokens are chosen so that lane
 //   L ends up with the logits of tokens 8 (L / 16) .. + 7 of head L % 16, which is just the operand that
 //   O^T += V^T P^T takes: neither product moves anything between lanes, and a page's V is laid out so that V^T is read as it lies.
@@ -13,36 +13,40 @@ namespace {
 // caches by (24 sequences of 2,000 to 4,096 tokens x 32 heads, pages of 16: 195 us, 217 without).  In larger pages a step's 64 bytes of a row of
 // V^T are half a line, and the wave with the other half wants it kept (130,001 tokens, pages of 64: 95 us, 107 if not); the
 // same holds for K, whose rows four instructions read in turn.
-template <bool BF16, int D, bool WHOLE_LINES, int kWaves>
+// TILES: more than 16 query heads share what is read of their key/value head (64 sequences of 4,096 to 8,192, 48 heads to one of 128: 63 us,
+// 115 a tile to a workgroup).
+template <bool BF16, int D, bool WHOLE_LINES, int kWaves, int TILES>
 __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void decode_kernel(const DecodeArgs A) {
   constexpr int KS = D / 32, DT = D / 16;
   const AttnArgs& a = A.a;
   const int part = blockIdx.z, s = blockIdx.y;
-  const int kvh = blockIdx.x / A.plan.tiles, tile = blockIdx.x - kvh * A.plan.tiles;
+  const int beside = (A.plan.tiles + TILES - 1) / TILES, kvh = blockIdx.x / beside, tile0 = (blockIdx.x - kvh * beside) * TILES;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int len = cached_tokens(a.c, s);
   const int begin = part * A.plan.chunk;
   if (begin >= len && part > 0) return;
   const int end = len - begin < A.plan.chunk ? len : begin + A.plan.chunk;
-  const int h0 = kvh * a.group + tile * kTileHeads;                 // first query head
-  const int cols = a.group - tile * kTileHeads < kTileHeads ? a.group - tile * kTileHeads : kTileHeads;
+  const int h0 = kvh * a.group + tile0 * kTileHeads;                // first query head
+  const int heads = a.group - tile0 * kTileHeads;                   // how many there are from it
   const int shift = a.c.page_shift, mask = (1 << shift) - 1;
 
-  u32x4 q[KS];
+  u32x4 q[TILES][KS];
 #pragma unroll
-  for (int k = 0; k < KS; ++k) q[k] = {0, 0, 0, 0};
-  if (col < cols) {
-    const uint16_t* row = a.q + s * a.qs.token + (h0 + col) * a.qs.head;
+  for (int n = 0; n < TILES; ++n) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) q[n][k] = {0, 0, 0, 0};
+    if (16 * n + col >= heads) continue;
+    const uint16_t* row = a.q + s * a.qs.token + (h0 + 16 * n + col) * a.qs.head;
     if (a.qs.dim == 1 && ((a.qs.token | a.qs.head) & 7) == 0) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) q[k] = *reinterpret_cast<const u32x4*>(row + 32 * k + 8 * g);
+      for (int k = 0; k < KS; ++k) q[n][k] = *reinterpret_cast<const u32x4*>(row + 32 * k + 8 * g);
     } else {
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int64_t d = 32 * k + 8 * g + 2 * i;
-          q[k][i] = row[d * a.qs.dim] | (uint32_t)row[(d + 1) * a.qs.dim] << 16;
+          q[n][k][i] = row[d * a.qs.dim] | (uint32_t)row[(d + 1) * a.qs.dim] << 16;
         }
     }
   }
@@ -55,8 +59,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
   u32x4 kf[2][KS], vf[DT];
   const int32_t* table = a.c.table + (int64_t)s * a.c.table_width;
   auto page_at = [&](int t) { return table[t >> shift < last_page ? t >> shift : last_page]; };
-  // (Behind the last step there is nothing to load: all lanes then read the buffer's first 16 bytes, so that the loop is one
-  // stretch of code in which every wait knows what is under way.)
+  // (Behind the last step there is nothing to load: all lanes then read the same 16 bytes of the buffer's first page, so that the loop
+  // is one stretch of code in which every wait knows what is under way.)
   auto load_k = [&](int t0, int page, bool there) {
     const uint16_t* base = a.k_pages + ((int64_t)page_inside(a.c, page) * a.c.kv_heads + kvh) * head_page + (((t0 + k_run) & mask) + k_in) * D + 8 * g;
     base = there ? base : a.k_pages;
@@ -79,10 +83,15 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
 
   // m: what the weights' exponents are taken from, the same in the four lanes of a head.  It follows the running maximum only
   // where a logit is more than kSlack above it (weights are then up to 2^(kLift + kSlack)): most steps scale nothing.
-  float m = -INFINITY, from = 0.f, l = 0.f;   // from: m, or 0 while m is -infinity
-  f32x4 o[DT];
+  float m[TILES], from[TILES], l[TILES];   // from: m, or 0 while m is -infinity
+  f32x4 o[TILES][DT];
 #pragma unroll
-  for (int i = 0; i < DT; ++i) o[i] = {0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < TILES; ++n) {
+    m[n] = -INFINITY;
+    from[n] = l[n] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[n][i] = {0.f, 0.f, 0.f, 0.f};
+  }
   constexpr int kStride = 32 * kWaves;
   int k_page = 0, v_page = 0;   // of the step after the one whose loads are under way: no load waits for the table
   int t0 = begin + 32 * wave;
@@ -96,106 +105,123 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
   }
   for (; t0 < end; t0 += kStride) {
     const bool more = t0 + kStride < end;
-    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+    f32x4 s0[TILES], s1[TILES];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      s0 = mfma16<BF16>(kf[0][k], q[k], s0);
-      s1 = mfma16<BF16>(kf[1][k], q[k], s1);
-    }
+    for (int n = 0; n < TILES; ++n) s0[n] = s1[n] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int n = 0; n < TILES; ++n) {
+        s0[n] = mfma16<BF16>(kf[0][k], q[n][k], s0[n]);
+        s1[n] = mfma16<BF16>(kf[1][k], q[n][k], s1[n]);
+      }
     __builtin_amdgcn_sched_barrier(0);   // into the registers that the products have just read, not into others before them
     load_k(t0 + kStride, k_page, more);
     k_page = page_at(t0 + 2 * kStride + k_run);
-    f32x8 x;
+    f32x8 x[TILES];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = s0[i] * a.scale_log2;
-      x[4 + i] = s1[i] * a.scale_log2;
-    }
+    for (int n = 0; n < TILES; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[n][i] = s0[n][i] * a.scale_log2;
+        x[n][4 + i] = s1[n][i] * a.scale_log2;
+      }
     if (t0 + 32 > len) {   // beyond the last token: no weight, and what is no number must not meet it
       const int rest = len - t0 - 8 * g;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = i < rest ? x[i] : -INFINITY;
+      for (int n = 0; n < TILES; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[n][i] = i < rest ? x[n][i] : -INFINITY;
       u32x4 keep;
 #pragma unroll
       for (int j = 0; j < 4; ++j) keep[j] = (2 * j < rest ? 0xffffu : 0u) | (2 * j + 1 < rest ? 0xffff0000u : 0u);
 #pragma unroll
       for (int i = 0; i < DT; ++i) vf[i] &= keep;
     }
-    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    if (__any(top > m + (kLift<BF16> + kSlack))) {
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float old = m;
-      m = fmaxf(m, top - kLift<BF16>);
-      from = m == -INFINITY ? 0.f : m;
-      const float shrink = exp2_fast(old - from);
-      l *= shrink;
 #pragma unroll
-      for (int i = 0; i < DT; ++i) o[i] *= shrink;
+    for (int n = 0; n < TILES; ++n) {
+      float top = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3])), fmaxf(fmaxf(x[n][4], x[n][5]), fmaxf(x[n][6], x[n][7])));
+      if (__any(top > m[n] + (kLift<BF16> + kSlack))) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float old = m[n];
+        m[n] = fmaxf(m[n], top - kLift<BF16>);
+        from[n] = m[n] == -INFINITY ? 0.f : m[n];
+        const float shrink = exp2_fast(old - from[n]);
+        l[n] *= shrink;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[n][i] *= shrink;
+      }
+      f32x8 p;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = exp2_fast(x[n][i] - from[n]);
+        l[n] += p[i];
+      }
+      const u32x4 pf = pack8<BF16>(p);
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[n][i] = mfma16<BF16>(vf[i], pf, o[n][i]);
     }
-    f32x8 p;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = exp2_fast(x[i] - from);
-      l += p[i];
-    }
-    const u32x4 pf = pack8<BF16>(p);
-#pragma unroll
-    for (int i = 0; i < DT; ++i) o[i] = mfma16<BF16>(vf[i], pf, o[i]);
     __builtin_amdgcn_sched_barrier(0);
     load_v(t0 + kStride, v_page, more);
     v_page = page_at(t0 + 2 * kStride + 8 * g);
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
 
   // The waves' sums, brought to one maximum: four values of a head a thread.
   constexpr int kThreads = 64 * kWaves;
   __shared__ float wave_m[kWaves][kTileHeads], wave_l[kWaves][kTileHeads];
   __shared__ __attribute__((aligned(16))) float wave_o[kWaves][kTileHeads * D];
   __shared__ uint32_t arrived;
-  if (g == 0) {
-    wave_m[wave][col] = m;
-    wave_l[wave][col] = l;
-  }
-  if (col < cols) {
-#pragma unroll
-    for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(&wave_o[wave][col * D + 16 * i + 4 * g]) = o[i];
-  }
-  __syncthreads();
-  const int parts = (len + A.plan.chunk - 1) / A.plan.chunk, quads = cols * (D / 4);
-  const int64_t unit = ((int64_t)s * a.c.kv_heads + kvh) * A.plan.tiles + tile;
+  const int parts = (len + A.plan.chunk - 1) / A.plan.chunk;
+  const int64_t unit = ((int64_t)s * a.c.kv_heads + kvh) * A.plan.tiles + tile0;
   const size_t part_size = part_floats(A.plan, D);
-  float* all = A.part + (size_t)unit * A.plan.parts * part_size;   // [part]: 16 maxima and sums of weights, cols x D sums over values
-  // out and lse of four values of head c; an empty row has no weights
-  auto finish = [&](int i, f32x4 sum, float top, float weight) {
-    const int c = i / (D / 4), d = 4 * (i % (D / 4));
-    uint16_t* to = a.out + s * a.os.token + (h0 + c) * a.os.head + d * a.os.dim;
+  // [tile][part]: 16 maxima and sums of weights, cols x D sums over values
+  auto parts_of = [&](int n) { return A.part + (size_t)(unit + n) * A.plan.parts * part_size; };
+  auto cols_of = [&](int n) { return heads - 16 * n < kTileHeads ? heads - 16 * n : kTileHeads; };   // 0 and less: no such tile
+  // out and lse of four values of head c of a tile; an empty row has no weights
+  auto finish = [&](int n, int i, f32x4 sum, float top, float weight) {
+    const int c = i / (D / 4), d = 4 * (i % (D / 4)), h = h0 + 16 * n + c;
+    uint16_t* to = a.out + s * a.os.token + h * a.os.head + d * a.os.dim;
 #pragma unroll
     for (int j = 0; j < 4; ++j) to[j * a.os.dim] = from_f32<BF16>(len > 0 ? sum[j] / weight : 0.f);
-    if (a.lse && d == 0) a.lse[(int64_t)s * a.heads + h0 + c] = len > 0 ? (top + __log2f(weight)) * 0.693147180559945f : -INFINITY;
+    if (a.lse && d == 0) a.lse[(int64_t)s * a.heads + h] = len > 0 ? (top + __log2f(weight)) * 0.693147180559945f : -INFINITY;
   };
-  for (int i = tid; i < quads; i += kThreads) {
-    const int c = i / (D / 4);
-    float top = wave_m[0][c];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_m[w][c]);
-    const float from = top == -INFINITY ? 0.f : top;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float weight = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = exp2_fast(wave_m[w][c] - from);
-      sum += f * *reinterpret_cast<const f32x4*>(&wave_o[w][4 * i]);
-      weight += f * wave_l[w][c];
+  for (int n = 0; n < TILES; ++n) {
+    float sum_l = l[n] + __shfl_xor(l[n], 16);
+    sum_l += __shfl_xor(sum_l, 32);
+    if (n > 0) __syncthreads();   // the tile before is read
+    if (g == 0) {
+      wave_m[wave][col] = m[n];
+      wave_l[wave][col] = sum_l;
     }
-    if (parts <= 1) {
-      finish(i, sum, top, weight);
-    } else {
-      float* mine = all + part * part_size;
-      shared_store(mine + 2 * kTileHeads + 4 * i, sum[0], sum[1]);
-      shared_store(mine + 2 * kTileHeads + 4 * i + 2, sum[2], sum[3]);
-      if (i % (D / 4) == 0) shared_store(mine + 2 * c, top, weight);
+    if (col < cols_of(n)) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(&wave_o[wave][col * D + 16 * i + 4 * g]) = o[n][i];
+    }
+    __syncthreads();
+    for (int i = tid; i < cols_of(n) * (D / 4); i += kThreads) {
+      const int c = i / (D / 4);
+      float top = wave_m[0][c];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_m[w][c]);
+      const float base = top == -INFINITY ? 0.f : top;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      float weight = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = exp2_fast(wave_m[w][c] - base);
+        sum += f * *reinterpret_cast<const f32x4*>(&wave_o[w][4 * i]);
+        weight += f * wave_l[w][c];
+      }
+      if (parts <= 1) {
+        finish(n, i, sum, top, weight);
+      } else {
+        float* mine = parts_of(n) + part * part_size;
+        shared_store(mine + 2 * kTileHeads + 4 * i, sum[0], sum[1]);
+        shared_store(mine + 2 * kTileHeads + 4 * i + 2, sum[2], sum[3]);
+        if (i % (D / 4) == 0) shared_store(mine + 2 * c, top, weight);
+      }
     }
   }
   if (parts <= 1) return;
@@ -208,122 +234,130 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
   if (arrived != (uint32_t)parts - 1) return;
   if (tid == 0) __hip_atomic_store(&A.counter[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   constexpr int kFew = 8;
-  if (parts <= kFew) {   // few: a thread asks for all it needs at once
-    for (int i = tid; i < quads; i += kThreads) {
-      f32x2 ml[kFew], v[kFew][2];
-#pragma unroll
-      for (int p = 0; p < kFew; ++p) {
-        const float* from = all + (p < parts ? p : 0) * part_size;
-        ml[p] = shared_load(from + 2 * (i / (D / 4)));
-        v[p][0] = shared_load(from + 2 * kTileHeads + 4 * i);
-        v[p][1] = shared_load(from + 2 * kTileHeads + 4 * i + 2);
-      }
-      float top = ml[0][0];
-#pragma unroll
-      for (int p = 1; p < kFew; ++p) top = fmaxf(top, ml[p][0]);
-      const float base = top == -INFINITY ? 0.f : top;
-      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-      float weight = 0.f;
-#pragma unroll
-      for (int p = 0; p < kFew; ++p) {
-        if (p >= parts) break;
-        const float f = exp2_fast(ml[p][0] - base);
-        sum += f * f32x4{v[p][0][0], v[p][0][1], v[p][1][0], v[p][1][1]};
-        weight += f * ml[p][1];
-      }
-      finish(i, sum, top, weight);
-    }
-    return;
-  }
-  // The parts' factors: thread (head tid % 16, every 16th part).
-  constexpr int kEach = (kMostParts + kThreads / kTileHeads - 1) / (kThreads / kTileHeads);
-  static_assert(kMostParts * kTileHeads <= kWaves * kTileHeads * D, "the factors fit where the waves' sums were");
-  float* factor = wave_o[0];                                        // [part][16]
   __shared__ float some[kThreads / kTileHeads][kTileHeads];
-  const int c0 = tid % kTileHeads, r0 = tid / kTileHeads;
-  float pm[kEach], pl[kEach];
-  float top = -INFINITY;
+  for (int n = 0; n < TILES && cols_of(n) > 0; ++n) {
+    const int cols = cols_of(n), quads = cols * (D / 4);
+    const float* all = parts_of(n);
+    if (parts <= kFew) {   // few: a thread asks for all it needs at once
+      for (int i = tid; i < quads; i += kThreads) {
+        f32x2 ml[kFew], v[kFew][2];
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) {
-    const int p = r0 + j * (kThreads / kTileHeads);
-    const bool there = p < parts && c0 < cols;
-    const f32x2 v = there ? shared_load(all + p * part_size + 2 * c0) : f32x2{-INFINITY, 0.f};
-    pm[j] = v[0];
-    pl[j] = v[1];
-  }
+        for (int p = 0; p < kFew; ++p) {
+          const float* from = all + (p < parts ? p : 0) * part_size;
+          ml[p] = shared_load(from + 2 * (i / (D / 4)));
+          v[p][0] = shared_load(from + 2 * kTileHeads + 4 * i);
+          v[p][1] = shared_load(from + 2 * kTileHeads + 4 * i + 2);
+        }
+        float top = ml[0][0];
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) top = fmaxf(top, pm[j]);
-  some[r0][c0] = top;
-  __syncthreads();
+        for (int p = 1; p < kFew; ++p) top = fmaxf(top, ml[p][0]);
+        const float base = top == -INFINITY ? 0.f : top;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        float weight = 0.f;
 #pragma unroll
-  for (int r = 0; r < kThreads / kTileHeads; ++r) top = fmaxf(top, some[r][c0]);
-  const float base = top == -INFINITY ? 0.f : top;
-  float weight = 0.f;
-#pragma unroll
-  for (int j = 0; j < kEach; ++j) {
-    const int p = r0 + j * (kThreads / kTileHeads);
-    const float f = exp2_fast(pm[j] - base);
-    weight += f * pl[j];
-    if (p < parts) factor[p * kTileHeads + c0] = f;
-  }
-  __syncthreads();
-  some[r0][c0] = weight;
-  if (r0 == 0) wave_m[0][c0] = top;
-  __syncthreads();
-  if (r0 == 0) {
-    weight = 0.f;
-#pragma unroll
-    for (int r = 0; r < kThreads / kTileHeads; ++r) weight += some[r][c0];
-    wave_l[0][c0] = weight;
-  }
-  __syncthreads();
-  // The sums: where there are fewer groups of four values than threads, several threads share one, each with every
-  // `share`th part.
-  const int share = quads < kThreads ? kThreads / quads : 1, mine = share > 1 ? tid / quads : 0;
-  f32x4* shared_sum = reinterpret_cast<f32x4*>(wave_o[0]);
-  for (int i0 = 0; i0 < quads; i0 += kThreads) {
-    const int i = share > 1 ? tid % quads : i0 + tid, c = i / (D / 4);
-    const bool busy = i < quads && mine < share;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (busy) {
-      const float* from_part = all + 2 * kTileHeads + 4 * i;
-      int p = mine;
-      for (; p + 7 * share < parts; p += 8 * share) {
-        f32x2 v[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = shared_load(from_part + (p + j / 2 * share) * part_size + j % 2 * 2);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += factor[(p + j * share) * kTileHeads + c] * f32x4{v[2 * j][0], v[2 * j][1], v[2 * j + 1][0], v[2 * j + 1][1]};
+        for (int p = 0; p < kFew; ++p) {
+          if (p >= parts) break;
+          const float f = exp2_fast(ml[p][0] - base);
+          sum += f * f32x4{v[p][0][0], v[p][0][1], v[p][1][0], v[p][1][1]};
+          weight += f * ml[p][1];
+        }
+        finish(n, i, sum, top, weight);
       }
-      for (; p < parts; p += share) {
-        const f32x2 u = shared_load(from_part + p * part_size), v = shared_load(from_part + p * part_size + 2);
-        sum += factor[p * kTileHeads + c] * f32x4{u[0], u[1], v[0], v[1]};
+      continue;
+    }
+    // The parts' factors: thread (head tid % 16, every 16th part).
+    constexpr int kEach = (kMostParts + kThreads / kTileHeads - 1) / (kThreads / kTileHeads);
+    static_assert(kMostParts * kTileHeads <= kWaves * kTileHeads * D, "the factors fit where the waves' sums were");
+    float* factor = wave_o[0];                                        // [part][16]
+    const int c0 = tid % kTileHeads, r0 = tid / kTileHeads;
+    float pm[kEach], pl[kEach];
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int p = r0 + j * (kThreads / kTileHeads);
+      const bool there = p < parts && c0 < cols;
+      const f32x2 v = there ? shared_load(all + p * part_size + 2 * c0) : f32x2{-INFINITY, 0.f};
+      pm[j] = v[0];
+      pl[j] = v[1];
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) top = fmaxf(top, pm[j]);
+    some[r0][c0] = top;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kThreads / kTileHeads; ++r) top = fmaxf(top, some[r][c0]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float weight = 0.f;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int p = r0 + j * (kThreads / kTileHeads);
+      const float f = exp2_fast(pm[j] - base);
+      weight += f * pl[j];
+      if (p < parts) factor[p * kTileHeads + c0] = f;
+    }
+    __syncthreads();
+    some[r0][c0] = weight;
+    if (r0 == 0) wave_m[0][c0] = top;
+    __syncthreads();
+    if (r0 == 0) {
+      weight = 0.f;
+#pragma unroll
+      for (int r = 0; r < kThreads / kTileHeads; ++r) weight += some[r][c0];
+      wave_l[0][c0] = weight;
+    }
+    __syncthreads();
+    // The sums: where there are fewer groups of four values than threads, several threads share one, each with every
+    // `share`th part.
+    const int share = quads < kThreads ? kThreads / quads : 1, mine = share > 1 ? tid / quads : 0;
+    f32x4* shared_sum = reinterpret_cast<f32x4*>(wave_o[0]);
+    for (int i0 = 0; i0 < quads; i0 += kThreads) {
+      const int i = share > 1 ? tid % quads : i0 + tid, c = i / (D / 4);
+      const bool busy = i < quads && mine < share;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      if (busy) {
+        const float* from_part = all + 2 * kTileHeads + 4 * i;
+        int p = mine;
+        for (; p + 7 * share < parts; p += 8 * share) {
+          f32x2 v[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = shared_load(from_part + (p + j / 2 * share) * part_size + j % 2 * 2);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum += factor[(p + j * share) * kTileHeads + c] * f32x4{v[2 * j][0], v[2 * j][1], v[2 * j + 1][0], v[2 * j + 1][1]};
+        }
+        for (; p < parts; p += share) {
+          const f32x2 u = shared_load(from_part + p * part_size), v = shared_load(from_part + p * part_size + 2);
+          sum += factor[p * kTileHeads + c] * f32x4{u[0], u[1], v[0], v[1]};
+        }
       }
+      if (share > 1) {   // quads < kThreads: one turn of the loop
+        __syncthreads();
+        if (busy) shared_sum[tid] = sum;
+        __syncthreads();
+        for (int r = 1; r < share && mine == 0; ++r) sum += shared_sum[r * quads + i];
+      }
+      if (busy && mine == 0) finish(n, i, sum, wave_m[0][c], wave_l[0][c]);
     }
-    if (share > 1) {   // quads < kThreads: one turn of the loop
-      __syncthreads();
-      if (busy) shared_sum[tid] = sum;
-      __syncthreads();
-      if (mine != 0) return;
-      for (int r = 1; r < share; ++r) sum += shared_sum[r * quads + i];
-    }
-    if (busy) finish(i, sum, wave_m[0][c], wave_l[0][c]);
+    __syncthreads();   // the next tile's numbers go where these were
   }
+}
+
+template <bool BF16, int D, bool WHOLE_LINES>
+void launch_pages(const DecodeArgs& a, dim3 grid, hipStream_t s) {
+  if constexpr (D <= kTogetherDim) {
+    if (a.plan.together == 3) return decode_kernel<BF16, D, WHOLE_LINES, 4, 3><<<grid, 256, 0, s>>>(a);
+    if (a.plan.together == 2) return decode_kernel<BF16, D, WHOLE_LINES, 4, 2><<<grid, 256, 0, s>>>(a);
+  }
+  if (a.plan.waves == 8) decode_kernel<BF16, D, WHOLE_LINES, 8, 1><<<grid, 512, 0, s>>>(a);
+  else decode_kernel<BF16, D, WHOLE_LINES, 4, 1><<<grid, 256, 0, s>>>(a);
 }
 
 template <bool BF16, int D>
 void launch_dim(const DecodeArgs& a, hipStream_t s) {
   // Workgroups go to the 8 XCDs in turn: with the heads first every XCD has as much of every sequence, whatever its length (parts
   // first, and 8 of them: the XCD of the last parts had nothing where sequences were short; 61 ragged ones 165 us, 77 so).
-  const dim3 grid(a.a.c.kv_heads * a.plan.tiles, a.a.c.n_seqs, a.plan.parts);
-  const bool whole = a.a.c.page_shift <= 5;
-  if (a.plan.waves == 8) {
-    if (whole) decode_kernel<BF16, D, true, 8><<<grid, 512, 0, s>>>(a);
-    else decode_kernel<BF16, D, false, 8><<<grid, 512, 0, s>>>(a);
-  } else {
-    if (whole) decode_kernel<BF16, D, true, 4><<<grid, 256, 0, s>>>(a);
-    else decode_kernel<BF16, D, false, 4><<<grid, 256, 0, s>>>(a);
-  }
+  const dim3 grid(a.a.c.kv_heads * ((a.plan.tiles + a.plan.together - 1) / a.plan.together), a.a.c.n_seqs, a.plan.parts);
+  if (a.a.c.page_shift <= 5) launch_pages<BF16, D, true>(a, grid, s);
+  else launch_pages<BF16, D, false>(a, grid, s);
 }
 
 template <bool BF16>

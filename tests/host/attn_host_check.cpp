@@ -63,6 +63,7 @@ hipError_t launch_attn_decode(const DecodeArgs& d, int head_dim, bool, hipStream
   REQUIRE(p.parts == 1 || (long long)p.chunk * (p.parts - 1) < a.c.max_len);
   REQUIRE((long long)p.chunk + a.c.max_len < 2147483647 - 1024);
   REQUIRE(p.cols >= 1 && p.cols <= kTileHeads && p.tiles * kTileHeads >= a.group && p.cols == (a.group < kTileHeads ? a.group : kTileHeads));
+  REQUIRE(p.together >= 1 && p.together <= 3 && (p.together == 1 || (head_dim <= kTogetherDim && p.waves == 4 && p.tiles > 1)));
   if (p.parts > 1) {   // the workspace holds the counters and every part
     const long long units = (long long)a.c.n_seqs * a.c.kv_heads * p.tiles;
     REQUIRE(units <= kJoinCounters);

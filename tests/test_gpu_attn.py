@@ -264,3 +264,12 @@ def test_a_prompt_is_what_its_tokens_are_one_at_a_time():
     torch.cuda.synchronize()
     assert (np.abs((got - out).double().cpu().numpy()) <= 2 * b_out).all()
     assert (np.abs((got_lse - lse).double().cpu().numpy()) <= 2 * b_lse).all()
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("heads, kv", [(17, 1), (32, 1), (40, 1), (48, 1), (64, 1), (100, 1), (96, 2)])
+def test_many_heads_to_one(heads, kv, dim):
+    """Several tiles of heads to a workgroup, with one part and with several; the last tile is not full."""
+    for lens in ([70, 0, 300, 1] * 6, [1300, 2] * 10):
+        p = Problem(heads, kv, dim, 64, "f16", lens, seed=heads, layout="features" if dim == 96 else "tokens")
+        p.check(*run(p, "decode"))
