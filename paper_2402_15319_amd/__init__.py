@@ -338,14 +338,15 @@ class AttnBatch:
                 raise ValueError("AttnBatch: max_len, or page_size to take what the table can list")
             max_len = page_table.shape[1] * page_size
         self.struct = VQAttnBatch(n, n_tokens, page_table.shape[1], max_len, _ptr(q_start) or None, _ptr(kv_len), _ptr(page_table))
+        self.n_tokens = n_tokens
         self._keep = (kv_len, page_table, q_start)
 
 
-def _rows(t, batch: AttnBatch, heads: int, desc: VQAttnDesc, what: str):
-    """The strides of a [n_tokens, heads, head_dim] tensor; None where it has no gaps."""
-    if t.dim() != 3 or t.shape[0] != batch.struct.n_tokens or t.shape[1] != heads or t.shape[2] != desc.head_dim or t.element_size() != 2:
-        raise ValueError(f"{what}: a 16-bit tensor [{batch.struct.n_tokens}, {heads}, {desc.head_dim}] is wanted, not {t.dtype} {tuple(t.shape)}")
-    return None if t.is_contiguous() else ctypes.byref(VQStrides(*t.stride()))
+def _rows(t, n: int, heads: int, dim: int, what: str):
+    """The strides of a [n, heads, dim] tensor; None where it has no gaps."""
+    if t.shape != (n, heads, dim) or t.element_size() != 2:
+        raise ValueError(f"{what}: a 16-bit tensor [{n}, {heads}, {dim}] is wanted, not {t.dtype} {tuple(t.shape)}")
+    return None if t.is_contiguous() else VQStrides(*t.stride())
 
 
 def vq_cache_bytes(desc: VQAttnDesc) -> int:
@@ -356,8 +357,9 @@ def vq_cache_bytes(desc: VQAttnDesc) -> int:
 
 def vq_cache_append(desc: VQAttnDesc, batch: AttnBatch, k, v, k_pages, v_pages, stream=None) -> None:
     """k, v: [n_tokens, kv_heads, head_dim] views (strides as vq_strides allows) of the new tokens."""
-    _check(lib().vq_cache_append(desc, batch.struct, _ptr(k), _rows(k, batch, desc.kv_heads, desc, "k"), _ptr(v),
-                                 _rows(v, batch, desc.kv_heads, desc, "v"), _ptr(k_pages), _ptr(v_pages), _stream(stream)), "vq_cache_append")
+    n, heads, dim = batch.n_tokens, desc.kv_heads, desc.head_dim
+    _check(lib().vq_cache_append(desc, batch.struct, k.data_ptr(), _rows(k, n, heads, dim, "k"), v.data_ptr(), _rows(v, n, heads, dim, "v"),
+                                 _ptr(k_pages), _ptr(v_pages), _stream(stream)), "vq_cache_append")
 
 
 def vq_cache_copy(desc: VQAttnDesc, buffers, from_to, stream=None) -> None:
@@ -366,7 +368,10 @@ def vq_cache_copy(desc: VQAttnDesc, buffers, from_to, stream=None) -> None:
         flat = array.array("i", [p for a, b in from_to for p in (a, b)])
     except (ValueError, TypeError, OverflowError) as e:
         raise ValueError("vq_cache_copy: from_to is a list of pairs of page numbers") from e
-    at = array.array("Q", [b if isinstance(b, int) else b.data_ptr() for b in buffers])
+    try:
+        at = array.array("Q", [b.data_ptr() for b in buffers])
+    except AttributeError:
+        at = array.array("Q", [_ptr(b) for b in buffers])
     _check(lib().vq_cache_copy(desc, len(at), at.buffer_info()[0], len(flat) // 2, flat.buffer_info()[0], _stream(stream)), "vq_cache_copy")
 
 
@@ -383,12 +388,11 @@ def attn_workspace(desc: VQAttnDesc, batch: AttnBatch, device="cuda:0"):
 
 
 def _attn(call, name, desc, batch, q, k_pages, v_pages, out, workspace, lse, stream):
-    if lse is not None and (lse.dim() != 2 or lse.shape[0] != q.shape[0] or lse.shape[1] != desc.heads or lse.element_size() != 4
-                            or not lse.is_contiguous()):
+    n, heads, dim = batch.n_tokens, desc.heads, desc.head_dim
+    if lse is not None and (lse.shape != (n, heads) or lse.element_size() != 4 or not lse.is_contiguous()):
         raise ValueError(f"{name}: lse is a contiguous float32 tensor [n_tokens, heads]")
-    _check(call(desc, batch.struct, _ptr(q), _rows(q, batch, desc.heads, desc, "q"), _ptr(k_pages), _ptr(v_pages), _ptr(out),
-                _rows(out, batch, desc.heads, desc, "out"), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                _stream(stream)), name)
+    _check(call(desc, batch.struct, q.data_ptr(), _rows(q, n, heads, dim, "q"), _ptr(k_pages), _ptr(v_pages), out.data_ptr(),
+                _rows(out, n, heads, dim, "out"), _ptr(lse), _ptr(workspace), workspace.nbytes, _stream(stream)), name)
 
 
 def vq_attn_decode(desc: VQAttnDesc, batch: AttnBatch, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:

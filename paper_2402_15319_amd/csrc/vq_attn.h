@@ -69,13 +69,12 @@ __host__ __device__ inline size_t part_floats(const DecodePlan& p, int head_dim)
 constexpr int kPromptRows = 128, kPromptTokens = 64;   // tokens: of a step
 constexpr int64_t kPromptMostWorkgroups = 1 << 20;
 
-// How a call of vq_attn_prompt is split: slots for tiles of 128 rows of a sequence, a row being a (new token, query head) pair, and parts of
-// at most so many steps.  A tile has `heads` query heads of one key/value head: all of the group, row after row those of a token, or, by
-// head, 1, 2 or 4 with 32 successive tokens of one head to a wave.
+// How a call of vq_attn_prompt is split: slots for tiles of one sequence's `tokens` new tokens and `heads` query heads of a
+// key/value head, 128 (token, head) rows or a few less, and parts of at most so many steps.
 struct PromptPlan {
   int64_t slots;
   int32_t steps, parts;
-  int32_t heads, by_head;
+  int32_t heads, tokens;
 };
 struct PromptArgs {
   AttnArgs a;

@@ -42,12 +42,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
       for (int k = 0; k < KS; ++k) q[n][k] = *reinterpret_cast<const u32x4*>(row + 32 * k + 8 * g);
     } else {
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t d = 32 * k + 8 * g + 2 * i;
-          q[n][k][i] = row[d * a.qs.dim] | (uint32_t)row[(d + 1) * a.qs.dim] << 16;
-        }
+      for (int k = 0; k < KS; ++k) q[n][k] = gather8(row + (32 * k + 8 * g) * a.qs.dim, a.qs.dim);
     }
   }
 

@@ -20,12 +20,12 @@ __device__ __forceinline__ int cached_tokens(const CacheArgs& c, int s) {
   return n < 0 ? 0 : n < c.max_len ? n : c.max_len;
 }
 
-// Work is handed out in tiles of `unit` rows of a sequence (a new token counts `each` rows), at most floor(rows / unit) + extra of
-// them.  Those of sequence i start at slot floor(first row / unit) + extra * i, which leaves room for the last ones of the sequences before;
+// Work is handed out in tiles of `unit` new tokens of a sequence, at most floor(tokens / unit) + extra of them.  Those of
+// sequence i start at slot floor(first token / unit) + extra * i, which leaves room for the last ones of the sequences before;
 // this is the sequence of a slot, the slot's number among its own, the sequence's rows (new tokens) first .. last - 1 and the tokens
 // in its cache, all inside the arrays whatever they hold.  A wave looks at 64 sequences at a time, with one wait for all of it.
 struct Tile { int sequence, number, first, last, cached; };
-__device__ __forceinline__ Tile tile_of(const CacheArgs& c, int slot, int each, int unit, int extra) {
+__device__ __forceinline__ Tile tile_of(const CacheArgs& c, int slot, int unit, int extra) {
   const int lane = threadIdx.x & 63;
   Tile t = {0, slot, 0, 0, 0};   // an empty sequence, where q_start does not begin with 0
   for (int base = 0; base < c.n_seqs; base += 64) {
@@ -34,7 +34,7 @@ __device__ __forceinline__ Tile tile_of(const CacheArgs& c, int slot, int each, 
     const int cached = cached_tokens(c, in);
     first = first < 0 ? 0 : first < c.n_tokens ? first : c.n_tokens;
     last = last < first ? first : last < c.n_tokens ? last : c.n_tokens;
-    const int at = first * each / unit + extra * i;
+    const int at = first / unit + extra * i;
     const int before = __popcll(__ballot(i < c.n_seqs && at <= slot));
     if (before == 0) break;
     t.sequence = base + before - 1;
@@ -58,6 +58,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+// Eight values `step` apart.
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ u32x4 gather8(const uint16_t* from, int64_t step) {
+  u16x8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = from[i * step];
+  return __builtin_bit_cast(u32x4, v);
+}
 
 // 16 x 16 += 16 x 32 . 32 x 16.  Lane L holds row (a) or column (b) L % 16 at k = 8 (L / 16) .. + 7, and of the result
 // column L % 16 at rows 4 (L / 16) .. + 3.

@@ -16,8 +16,8 @@ template <int D> __device__ __forceinline__ int k_turn(int r) {
   return D % 128 == 0 ? r & 15 : D == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
 }
 
-// One workgroup: 128 rows of one sequence and one key/value head, a row being a (new token, query head of the group) pair, 32 a
-// wave, and all tokens that they attend (or a part of them), 64 at a time.
+// One workgroup: up to 128 rows of one sequence and one key/value head, a row being a (new token, query head of the group) pair, 32
+// a wave, and all tokens that they attend (or a part of them), 64 at a time.
 //   S^T = K Q^T, O^T += V^T P^T, 32 x 32 x 16: a lane has one row's logits (half of a step's), weights and sums, so that a row's
 //   maximum and sum need the other half-wave only, and P goes from the first product's registers into the second's as
 //   it is: row m of the first operand is token m with bits 2 and 3 exchanged, which leaves a lane with eight successive tokens.
@@ -34,33 +34,21 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
   // first: they attend most.
   const int group = a.group, heads_in = A.plan.heads, wide = a.heads / heads_in;   // query heads of a tile; tiles beside one another
   const int slot = (int)A.plan.slots - 1 - blockIdx.x / wide, beside = blockIdx.x % wide, head0 = beside * heads_in, kvh = head0 / group;
-  const Tile tile = tile_of(a.c, slot, heads_in, kRows, 1);
+  const int tokens = A.plan.tokens;
+  const Tile tile = tile_of(a.c, slot, tokens, 1);
   const int s = tile.sequence, first = tile.first, n = tile.last - first, len = tile.cached, behind = len - n;   // new token i: position behind + i
-  if (tile.number * kRows >= n * heads_in) return;
-  // The wave's rows: tokens low .. high of its heads (none if low >= n), and the lane's: (token, head), valid or the last one again.
-  int token, head, low, high, most;
-  bool valid;
-  if (A.plan.by_head) {   // 32 tokens of one head
-    const int tokens = kRows / heads_in, at = 32 * wave;
-    low = tile.number * tokens + at % tokens;
-    high = low + 31 < n ? low + 31 : n - 1;
-    most = tile.number * tokens + tokens - 1;
-    token = low + col;
-    head = head0 + at / tokens;
-    valid = token < n;
-  } else {                // all heads of a token after the other
-    const int row = tile.number * kRows + 32 * wave, end = n * heads_in - 1;
-    low = row / heads_in;
-    high = (row + 31 < end ? row + 31 : end) / heads_in;
-    most = (tile.number * kRows + kRows - 1) / heads_in;
-    valid = row + col <= end;
-    const int mine = valid ? row + col : end;
-    token = mine / heads_in;
-    head = head0 + mine - token * heads_in;
-    low = row <= end ? low : n;
-  }
-  token = token < n ? token : n - 1;
-  most = behind + (most < n ? most : n - 1);
+  const int token0 = tile.number * tokens;
+  if (token0 >= n) return;
+  // Row r is token r % tokens of head r / tokens.  The wave's are tokens low .. high (none if low >= n), the lane's one is valid or
+  // works on some other.
+  const int row = 32 * wave, end = heads_in * tokens - 1, row1 = row + 31 < end ? row + 31 : end;
+  const bool one_head = row <= end && row / tokens == row1 / tokens;
+  const int low = row > end ? n : token0 + (one_head ? row % tokens : 0), last = token0 + (one_head ? row1 % tokens : tokens - 1);
+  const int high = last < n ? last : n - 1;
+  const int mine = row + col <= end ? row + col : end, token_in = token0 + mine % tokens, token = token_in < n ? token_in : n - 1;
+  const int head = head0 + mine / tokens;
+  const bool valid = row + col <= end && token_in < n;
+  const int most = behind + (token0 + tokens < n ? token0 + tokens : n) - 1;   // highest position of the tile
   const int pos = behind + token, wave_first = behind + low, wave_last = low < n ? behind + high : -1;
   const int all = most < 0 ? 0 : most / kTokens + 1;       // steps of the tile, and this part's: begin .. steps - 1
   const int begin = blockIdx.y * A.plan.steps, steps = all - begin < A.plan.steps ? all : begin + A.plan.steps;
@@ -92,12 +80,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
       for (int k = 0; k < KS; ++k) q[k] = *reinterpret_cast<const u32x4*>(from + 16 * k + 8 * half);
     } else {
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t d = 16 * k + 8 * half + 2 * i;
-          q[k][i] = from[d * a.qs.dim] | (uint32_t)from[(d + 1) * a.qs.dim] << 16;
-        }
+      for (int k = 0; k < KS; ++k) q[k] = gather8(from + (16 * k + 8 * half) * a.qs.dim, a.qs.dim);
     }
   }
 

@@ -28,26 +28,18 @@ __device__ __forceinline__ int64_t head_of(const CacheArgs& c, int s, int pos, i
 // A token at a time: a thread takes eight dimensions of a head's key and value.
 __global__ __launch_bounds__(256) void append_one_kernel(const AppendArgs a, int head_dim) {
   const int t = blockIdx.x, pieces = head_dim / 8, i = blockIdx.y * 256 + threadIdx.x, h = i / pieces, d = 8 * (i - h * pieces);
-  const Tile tile = a.c.q_start ? tile_of(a.c, t, 1, 1, 0) : Tile{t, 0, t, t + 1, cached_tokens(a.c, t)};
+  const Tile tile = a.c.q_start ? tile_of(a.c, t, 1, 0) : Tile{t, 0, t, t + 1, cached_tokens(a.c, t)};
   const int s = tile.sequence, pos = tile.cached - tile.last + t;
   if (h >= a.c.kv_heads || t < tile.first || t >= tile.last || pos < 0) return;
   const int size = 1 << a.c.page_shift, slot = pos & (size - 1);
   const uint16_t* k = a.k + t * a.ks.token + h * a.ks.head + d * a.ks.dim;
   const uint16_t* v = a.v + t * a.vs.token + h * a.vs.head + d * a.vs.dim;
-  uint16_t kx[8], vx[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    kx[j] = k[j * a.ks.dim];
-    vx[j] = v[j * a.vs.dim];
-  }
+  const u32x4 kx = gather8(k, a.ks.dim), vx = gather8(v, a.vs.dim);
   const int64_t base = head_of(a.c, s, pos, h, head_dim);
   if (base < 0) return;
-  u32x4 row;
+  *reinterpret_cast<u32x4*>(a.k_pages + base + slot * head_dim + d) = kx;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) row[j] = kx[2 * j] | (uint32_t)kx[2 * j + 1] << 16;
-  *reinterpret_cast<u32x4*>(a.k_pages + base + slot * head_dim + d) = row;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) a.v_pages[base + (int64_t)(d + j) * size + slot] = vx[j];
+  for (int j = 0; j < 8; ++j) a.v_pages[base + (int64_t)(d + j) * size + slot] = (uint16_t)(vx[j / 2] >> (j % 2 * 16));
 }
 
 // Any number of new tokens: a workgroup takes 64 positions of a sequence and a head, half of its waves the keys and half the
@@ -60,7 +52,7 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const App
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool values = wave >= kHalves;
   const int h = blockIdx.x % a.c.kv_heads;
-  const Tile tile = tile_of(a.c, blockIdx.x / a.c.kv_heads, 1, kTile, 2);
+  const Tile tile = tile_of(a.c, blockIdx.x / a.c.kv_heads, kTile, 2);
   const int s = tile.sequence, first = tile.first, last = tile.last;
   const int behind = tile.cached - last, from = behind + first > 0 ? behind + first : 0;   // token t has position behind + t
   // lanes: positions first where the source runs along them, dimensions first where it runs along those
@@ -91,8 +83,7 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const App
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint16_t* row = src + (i < lo ? lo : i < hi ? i : hi - 1) * st.token;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) in[i][j] = row[2 * j * dim] | (uint32_t)row[(2 * j + 1) * dim] << 16;
+      in[i] = gather8(row, dim);
     }
   }
   if (by_token == values) {

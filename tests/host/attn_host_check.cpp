@@ -78,8 +78,8 @@ hipError_t launch_attn_prompt(const PromptArgs& d, int head_dim, bool, hipStream
   const PromptPlan& p = d.plan;
   check_attn(a, head_dim);
   // a slot for every tile, every step in a part, no part that the longest sequence leaves empty
-  REQUIRE(p.heads >= 1 && a.group % p.heads == 0 && (p.by_head ? p.heads == 1 || p.heads == 2 || p.heads == 4 : p.heads == a.group));
-  REQUIRE(p.slots == (long long)a.c.n_tokens * p.heads / kPromptRows + a.c.n_seqs);
+  REQUIRE(p.heads >= 1 && a.group % p.heads == 0 && p.tokens >= 1 && p.heads * p.tokens <= kPromptRows);
+  REQUIRE(p.slots == a.c.n_tokens / p.tokens + a.c.n_seqs);
   const long long wide = a.heads / p.heads;
   REQUIRE(p.slots * wide * 256 < 4294967296ll);
   REQUIRE(p.steps >= 1 && p.parts >= 1 && p.parts <= 65535 && (long long)p.steps * p.parts * kPromptTokens >= a.c.max_len);
@@ -89,7 +89,7 @@ hipError_t launch_attn_prompt(const PromptArgs& d, int head_dim, bool, hipStream
     const size_t end = (size_t)((char*)d.part - (char*)d.counter) + (size_t)p.slots * wide * p.parts * prompt_part_floats(head_dim) * 4;
     REQUIRE((char*)d.part - (char*)d.counter >= kJoinCounters * 4 && end <= g_workspace);
   }
-  REQUIRE((long long)a.c.n_tokens * a.group + kPromptRows < 2147483647);   // rows of a key/value head
+  REQUIRE((long long)a.c.n_tokens + a.c.n_seqs + kPromptRows < 2147483647);
   return hipSuccess;
 }
 }  // namespace vq
