@@ -70,11 +70,11 @@ constexpr int kPromptRows = 128, kPromptTokens = 64;   // tokens: of a step
 constexpr int64_t kPromptMostWorkgroups = 1 << 20;
 
 // How a call of vq_attn_prompt is split: slots for tiles of one sequence's `tokens` new tokens and `heads` query heads of a
-// key/value head, 128 (token, head) rows or a few less, and parts of at most so many steps.
+// key/value head, 128 (token, head) rows or a few less, and parts of at most so many steps, which one or two teams of four waves take in turn.
 struct PromptPlan {
   int64_t slots;
   int32_t steps, parts;
-  int32_t heads, tokens;
+  int32_t heads, tokens, teams;
 };
 struct PromptArgs {
   AttnArgs a;

@@ -126,7 +126,6 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   return p;
 }
 
-constexpr int64_t kEnoughTiles = 512;   // workgroups
 constexpr int kLeastSteps = 8;          // of a part
 
 PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
@@ -149,7 +148,18 @@ PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   p.tokens = (int32_t)(2 * mean < kPromptRows / p.heads ? 2 * mean : kPromptRows / p.heads);
   p.slots = b.n_tokens / p.tokens + b.n_seqs;
   const int64_t units = p.slots * (d.heads / p.heads), steps = b.max_len > 0 ? ((int64_t)b.max_len + kPromptTokens - 1) / kPromptTokens : 1;
-  int64_t parts = units < kEnoughTiles ? (kEnoughTiles + units - 1) / units : 1;
+  // Two workgroups of one team share a compute unit and run a step each in about 2.1 us; one alone takes 1.3 us a step.  Where there is but
+  // one for each compute unit, or where two are gone through long before the last, two teams take a tile's steps in turn.  Theirs is one
+  // barrier, which keeps both at the same work and costs a long prompt 14 %.  Three workgroups on heads of 64 share a compute unit: those keep
+  // one team where parts are long.  (32 heads of 128, prompts of 768, 1,024 and 1,500: 24.6, 29.3 and 40.0 us with one team, 20.4, 24.9 and
+  // 36.1 with two; two chunks behind 12,000 tokens, heads of 64: 72 us with one, 96 with two.)
+  const int64_t full = (b.n_tokens + (int64_t)p.tokens - 1) / p.tokens * (d.heads / p.heads);   // tiles, but for those that a sequence does not fill
+  const bool lone = full <= 256 && steps >= 8 && (steps <= 32 || d.head_dim > 64), few = full <= 512 && steps >= 24 && steps <= 32;
+  p.teams = d.head_dim <= 128 && (lone || few) ? 2 : 1;
+  // Parts, where they bring the workgroups near to what the chip runs at once (heads of 256 have one workgroup to a compute unit, and of
+  // longer parts: 16 heads, 1,500 and 2,048 tokens 67 and 88 us whole, 51 and 80 in two parts).
+  const int64_t enough = p.teams == 2 ? 256 : d.head_dim > 128 ? 448 : 512;
+  int64_t parts = units < enough ? (enough + units / 2) / units : 1;
   while (parts > 1 && parts * parts > steps) --parts;   // to join a part takes about as long as a step
   int64_t per = (steps + parts - 1) / parts;
   per = per < kLeastSteps ? kLeastSteps : per;

@@ -7,7 +7,7 @@
 namespace vq {
 namespace {
 
-constexpr int kWaves = 4, kRows = kPromptRows, kTokens = kPromptTokens;   // rows of a workgroup's tile; tokens of a step
+constexpr int kWaves = 4 /* of a team */, kRows = kPromptRows, kTokens = kPromptTokens;   // rows of a workgroup's tile; tokens of a step
 static_assert(kRows == 32 * kWaves, "32 rows a wave");
 
 // 16-byte pieces of a row of K in LDS change places so that 16 rows' pieces of one number lie in different banks: piece p of row r
@@ -22,14 +22,15 @@ template <int D> __device__ __forceinline__ int k_turn(int r) {
 //   maximum and sum need the other half-wave only, and P goes from the first product's registers into the second's as
 //   it is: row m of the first operand is token m with bits 2 and 3 exchanged, which leaves a lane with eight successive tokens.
 // K and V^T of a step come into LDS past the registers, each wave 16 tokens of both (one page), while the step before is
-// worked on.
-template <bool BF16, int D>
-__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(const PromptArgs A) {
+// worked on.  With two teams of such waves (see the plan) each takes every second step, and the second's sums go to the first in the end.
+template <bool BF16, int D, int TEAMS>
+__global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_kernel(const PromptArgs A) {
   const AttnArgs& a = A.a;
   constexpr int KS = D / 16, DT = D / 32, kLoads = D / 32;     // loads of a wave for its 16 tokens' K, and for their V
   constexpr int kHalf = kTokens * D * 2, kStep = 2 * kHalf;    // bytes of K, or V, of a step
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kStep];
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
+  __shared__ __attribute__((aligned(1024))) char lds[TEAMS * 2 * kStep];
+  const int tid = threadIdx.x, number = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
+  const int wave = number % kWaves, team = number / kWaves;
   // The heads are neighbours, and so are on the 8 XCDs in turn: those of an XCD keep to their keys and values.  Of the tiles the last come
   // first: they attend most.
   const int group = a.group, heads_in = A.plan.heads, wide = a.heads / heads_in;   // query heads of a tile; tiles beside one another
@@ -64,14 +65,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
     k_off[j] = (r * D + (p ^ k_turn<D>(r)) * 8) * 2;
   }
   const uint32_t v_off = (((lane >> 1) << shift) + 8 * ((lane & 1) ^ ((lane >> 4) & 1))) * 2;
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds) + team * (2 * kStep);
   const int32_t* table = a.c.table + (int64_t)s * a.c.table_width;
-  // Lane i: the wave's page in step begin + i (mod 64) of the 64 that are being loaded; asked for before q, which the loads need not wait for.
+  // Lane i: the wave's page in the i-th (mod 64) of the steps that are being loaded; asked for before q, which the loads need not wait for.
   auto pages_from = [&](int step) {
-    const int j = ((step + lane) * kTokens + 16 * wave) >> shift;
+    const int j = ((step + TEAMS * lane) * kTokens + 16 * wave) >> shift;
     return table[j < last_page ? j : last_page];
   };
-  int pages = pages_from(begin);
+  int pages = pages_from(begin + team);
   u32x4 q[KS];
   {
     const uint16_t* from = a.q + (int64_t)(first + token) * a.qs.token + head * a.qs.head;
@@ -85,21 +86,21 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
   }
 
   auto load = [&](int step) {
-    const int at = (step - begin) & 63;
-    if (at == 0 && step > begin) pages = pages_from(step);
+    const int at = ((step - begin) / TEAMS) & 63;
+    if (at == 0 && step >= begin + TEAMS) pages = pages_from(step);
     const int page = page_inside(a.c, __builtin_amdgcn_readlane(pages, at));
     const int in = (step * kTokens + 16 * wave) & mask;
     const int64_t page_head = ((int64_t)page * a.c.kv_heads + kvh) * ((int64_t)D << shift);
     const uint16_t* k = a.k_pages + page_head + in * D;
     const uint16_t* v = a.v_pages + page_head + in;
-    const uint32_t to = lds0 + (step & 1) * kStep + wave * (kHalf / kWaves);
+    const uint32_t to = lds0 + ((step / TEAMS) & 1) * kStep + wave * (kHalf / kWaves);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) load_to_lds(k, k_off[j], to + 1024 * j);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) load_to_lds(v + ((int64_t)(32 * j) << shift), v_off, to + kHalf + 1024 * j);
   };
 
-  int step = begin;
+  int step = begin + team;
   if (step < steps) load(step);
 #pragma unroll
   for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));   // here, or the compiler waits for them in the loop, and with them for its loads
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
 
   auto work = [&](int step, auto masked_) {
     constexpr bool masked = decltype(masked_)::value;
-    const char* kt = lds + (step & 1) * kStep;
+    const char* kt = lds + (2 * team + ((step / TEAMS) & 1)) * kStep;
     const char* vt = kt + kHalf;
     f32x16 x[2];
     // The products of the logits go before another wave's weights (nine packed prompts 94 to 95 us, 98 without).
@@ -227,21 +228,50 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
 
   // First the steps whose tokens all of the wave's rows attend.
   const int whole = low < n && wave_first >= 0 ? (wave_first + 1) / kTokens : 0;
-  for (; step < whole && step < steps; ++step) {
+  for (; step < whole && step < steps; step += TEAMS) {
     lds_turn();
-    if (step + 1 < steps) load(step + 1);
+    if (step + TEAMS < steps) load(step + TEAMS);
     work(step, std::false_type());
   }
-  for (; step < steps; ++step) {
+  for (; step - team < steps; step += TEAMS) {
     lds_turn();
-    if (step + 1 < steps) load(step + 1);
-    if (step * kTokens <= wave_last) work(step, std::true_type());
+    if (step + TEAMS < steps) load(step + TEAMS);
+    if ((TEAMS == 1 || step < steps) && step * kTokens <= wave_last) work(step, std::true_type());
   }
 
   l += __shfl_xor(l, 32);
+  if constexpr (TEAMS == 2) {
+    // What the second team has goes through LDS, [maximum and sum of the weights, then four sums over values at a time][lane].
+    constexpr int kPieces = 1 + 4 * DT;
+    static_assert(kWaves * kPieces * 1024 <= (int)sizeof(lds));
+    f32x4* at = reinterpret_cast<f32x4*>(lds) + wave * (kPieces * 64) + lane;
+    __syncthreads();
+    if (team == 1) {
+      at[0] = f32x4{m, l, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4 * DT; ++i)
+        at[(1 + i) * 64] = f32x4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2], o[i >> 2][4 * (i & 3) + 3]};
+    }
+    __syncthreads();
+    if (team == 1) return;
+    const f32x4 ml = at[0];
+    const float old = m;
+    m = fmaxf(m, ml[0]);
+    const float base = m == -INFINITY ? 0.f : m, f0 = exp2_fast(old - base), f1 = exp2_fast(ml[0] - base);
+    l = f0 * l + f1 * ml[1];
+#pragma unroll
+    for (int i = 0; i < 4 * DT; ++i) {
+      const f32x4 v = at[(1 + i) * 64];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o[i >> 2][4 * (i & 3) + j] = f0 * o[i >> 2][4 * (i & 3) + j] + f1 * v[j];
+      }
+    }
+  }
   const int parts = (all + A.plan.steps - 1) / A.plan.steps;
   if (parts > 1) {
-    // Whoever finishes last joins the parts, in their order.  A lane's numbers lie where the same lane finds them: [part][maximum and sum
+    // Whoever finishes last joins the parts, in their order; a part's loads are under way together (a wait for each took 25 us of 63, 256
+    // dimensions).  A lane's numbers lie where the same lane finds them: [part][maximum and sum
     // of the weights, then two sums over values at a time][lane].
     __shared__ uint32_t arrived;
     constexpr int kPairs = 1 + 8 * DT;
@@ -264,8 +294,6 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
     if (tid == 0) __hip_atomic_store(&A.counter[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (low >= n) return;
     m = -INFINITY;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, shared_load(mine + p * kPart)[0]);
-    const float base = m == -INFINITY ? 0.f : m;
     l = 0.f;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -273,17 +301,31 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
       for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
     for (int p = 0; p < parts; ++p) {
       const float* of = mine + p * kPart;
+      constexpr int kAhead = D == 256 ? 16 : 8 * DT;   // loads under way together
       const f32x2 ml = shared_load(of);
-      const float f = exp2_fast(ml[0] - base);
-      l += f * ml[1];
+      f32x2 v[kAhead];
+      float old = 0.f, now = 0.f;
 #pragma unroll
-      for (int i = 0; i < DT; ++i)
+      for (int at = 0; at < 8 * DT; at += kAhead) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const f32x2 v = shared_load(of + (1 + 8 * i + j) * 128);
-          o[i][2 * j] += f * v[0];
-          o[i][2 * j + 1] += f * v[1];
+        for (int j = 0; j < kAhead; ++j) v[j] = shared_load(of + (1 + at + j) * 128);
+        __builtin_amdgcn_sched_barrier(0);
+        if (at == 0) {
+          const float top = fmaxf(m, ml[0]), base = top == -INFINITY ? 0.f : top;
+          old = exp2_fast(m - base);
+          now = exp2_fast(ml[0] - base);
+          m = top;
+          l = old * l + now * ml[1];
         }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int d = 2 * (at + j) + e;
+            o[d >> 4][d & 15] = old * o[d >> 4][d & 15] + now * v[j][e];
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
   const bool any = pos >= 0;
@@ -321,7 +363,13 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_kernel(c
 
 template <bool BF16, int D>
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t s) {
-  prompt_kernel<BF16, D><<<dim3((unsigned)(a.a.heads / a.plan.heads * a.plan.slots), a.plan.parts), 64 * kWaves, 0, s>>>(a);
+  const dim3 grid((unsigned)(a.a.heads / a.plan.heads * a.plan.slots), a.plan.parts);
+  if constexpr (D <= 128)
+    if (a.plan.teams == 2) {
+      prompt_kernel<BF16, D, 2><<<grid, 2 * 64 * kWaves, 0, s>>>(a);
+      return hipGetLastError();
+    }
+  prompt_kernel<BF16, D, 1><<<grid, 64 * kWaves, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -273,3 +273,35 @@ def test_many_heads_to_one(heads, kv, dim):
     for lens in ([70, 0, 300, 1] * 6, [1300, 2] * 10):
         p = Problem(heads, kv, dim, 64, "f16", lens, seed=heads, layout="features" if dim == 96 else "tokens")
         p.check(*run(p, "decode"))
+
+
+@pytest.mark.parametrize("dim, page, dtype", [(64, 16, "f16"), (64, 128, "bf16"), (96, 32, "f16"), (96, 16, "bf16"), (128, 64, "f16"), (128, 16, "bf16"), (256, 32, "f16")])
+@pytest.mark.parametrize("lens, new", [([449], [449]), ([513], [513]), ([1000], [777]), ([1600], [1600]), ([0, 700, 1, 450], [0, 700, 1, 450]),
+                                       ([1500, 30, 0, 640], [130, 30, 3, 1]), ([5000], [40]), ([2040, 500], [1, 520])])
+def test_middling_prompts_on_few_heads(dim, page, dtype, lens, new):
+    """Few tiles of 8 to 80 steps each: odd and even numbers of steps, rows without tokens, sequences that are much shorter than the longest."""
+    p = Problem(4, 2, dim, page, dtype, lens, new=new, layout="features" if page == 16 else "tokens", seed=sum(lens))
+    out, lse = run(p)
+    p.check(out, lse)
+    again, _ = run(p)
+    assert bool((out == again).all())
+
+
+@pytest.mark.parametrize("where, value", [("k", np.inf), ("v", np.nan), ("v", -np.inf)])
+def test_what_is_no_number_in_middling_prompts(where, value):
+    """It goes to the rows that attend it and no other, from whichever half of the steps."""
+    p = Problem(4, 2, 128, 16, "f16", [700], new=[700], seed=9)
+    for token in (70, 330, 699):
+        at = int(p.table[0, token // 16]), token % 16
+        if where == "k":
+            p.k_host[at[0], 1, at[1], :] = value
+        else:
+            p.v_host[at[0], 1, 3, at[1]] = value
+    p.k_pages, p.v_pages = p.k_host.to(p.dev), p.v_host.to(p.dev)
+    got = run(p)[0].double().cpu().numpy()
+    ref = p.reference()
+    assert np.array_equal(np.isfinite(got), np.isfinite(ref[0]))
+    b_out, _ = p.bounds(ref)
+    with np.errstate(invalid="ignore"):
+        over = (np.abs(got - ref[0]) > b_out) & np.isfinite(ref[0]) & np.isfinite(b_out)
+    assert not over.any()
