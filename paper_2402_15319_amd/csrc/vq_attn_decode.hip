@@ -31,18 +31,29 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
   const int shift = a.c.page_shift, mask = (1 << shift) - 1;
 
   u32x4 q[TILES][KS];
+  const bool whole_rows = a.qs.dim == 1 && ((a.qs.token | a.qs.head) & 7) == 0;
+  // Any other order: each value is fetched once for the workgroup and goes through LDS (61 sequences, 8 heads to a key/value head, the
+  // tokens next to one another: 66 us, 79 with every wave fetching all).
+  constexpr int kRow = D + 8;   // of q in LDS: 16 rows' pieces in different banks
+  __shared__ __attribute__((aligned(16))) uint16_t q_rows[TILES * kTileHeads * kRow];
+  if (!whole_rows) {
+    const int rows = heads < TILES * kTileHeads ? heads : TILES * kTileHeads;
+    const uint16_t* at = a.q + s * a.qs.token + h0 * a.qs.head;
+    for (int i = tid; i < rows * D; i += 64 * kWaves) q_rows[i / D * kRow + i % D] = at[i / D * a.qs.head + i % D * a.qs.dim];
+    __syncthreads();
+  }
 #pragma unroll
   for (int n = 0; n < TILES; ++n) {
 #pragma unroll
     for (int k = 0; k < KS; ++k) q[n][k] = {0, 0, 0, 0};
     if (16 * n + col >= heads) continue;
-    const uint16_t* row = a.q + s * a.qs.token + (h0 + 16 * n + col) * a.qs.head;
-    if (a.qs.dim == 1 && ((a.qs.token | a.qs.head) & 7) == 0) {
+    if (whole_rows) {
+      const uint16_t* row = a.q + s * a.qs.token + (h0 + 16 * n + col) * a.qs.head;
 #pragma unroll
       for (int k = 0; k < KS; ++k) q[n][k] = *reinterpret_cast<const u32x4*>(row + 32 * k + 8 * g);
     } else {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) q[n][k] = gather8(row + (32 * k + 8 * g) * a.qs.dim, a.qs.dim);
+      for (int k = 0; k < KS; ++k) q[n][k] = *reinterpret_cast<const u32x4*>(&q_rows[(16 * n + col) * kRow + 32 * k + 8 * g]);
     }
   }
 
