@@ -113,7 +113,8 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   } else if (units * p.together <= kJoinCounters) {
     // A workgroup for every CU is enough where they are of one size (130,001 tokens x 8 heads: 256 workgroups 97 us, 512 100,
     // 1,024 106).  Where there are as many without a split, the lengths will differ, and parts of 1,024 tokens even them
-    // out (61 sequences of 1 to 8,192: parts of 1,024 68 us, of 2,048 77, of 4,096 85; 24 of 2,048 to 4,096 alike: 203 and 202).
+    // out (61 sequences of 1 to 8,192: parts of 512 61 us, of 1,024 66, before q came through LDS 68, of 2,048 77 then; 61 of 4,000 each:
+    // parts of 512 194 us, of 1,024 177).
     const int64_t most = units < kEnoughUnits ? kLongPart : kShortPart;
     const int64_t enough = (kEnoughUnits + units - 1) / units, least = (steps * kPartStep + most - 1) / most;
     parts = (least + enough - 1) / enough * enough;   // as many for every CU
