@@ -84,6 +84,7 @@ hipError_t launch_attn_prompt(const PromptArgs& d, int head_dim, bool, hipStream
   REQUIRE(p.slots * wide * 256 < 4294967296ll);
   REQUIRE(p.steps >= 1 && p.parts >= 1 && p.parts <= 65535 && (long long)p.steps * p.parts * kPromptTokens >= a.c.max_len);
   REQUIRE(p.parts == 1 || (long long)p.steps * (p.parts - 1) * kPromptTokens < a.c.max_len);
+  REQUIRE(p.teams == 1 || (p.teams == 2 && head_dim <= 128));
   if (p.parts > 1) {
     REQUIRE(p.slots * wide <= kJoinCounters);
     const size_t end = (size_t)((char*)d.part - (char*)d.counter) + (size_t)p.slots * wide * p.parts * prompt_part_floats(head_dim) * 4;
