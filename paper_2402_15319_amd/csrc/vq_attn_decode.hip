@@ -42,20 +42,23 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
     for (int i = tid; i < rows * D; i += 64 * kWaves) q_rows[i / D * kRow + i % D] = at[i / D * a.qs.head + i % D * a.qs.dim];
     __syncthreads();
   }
+  auto load_q = [&]() {
 #pragma unroll
-  for (int n = 0; n < TILES; ++n) {
+    for (int n = 0; n < TILES; ++n) {
 #pragma unroll
-    for (int k = 0; k < KS; ++k) q[n][k] = {0, 0, 0, 0};
-    if (16 * n + col >= heads) continue;
-    if (whole_rows) {
-      const uint16_t* row = a.q + s * a.qs.token + (h0 + 16 * n + col) * a.qs.head;
+      for (int k = 0; k < KS; ++k) q[n][k] = {0, 0, 0, 0};
+      if (16 * n + col >= heads) continue;
+      if (whole_rows) {
+        const uint16_t* row = a.q + s * a.qs.token + (h0 + 16 * n + col) * a.qs.head;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) q[n][k] = *reinterpret_cast<const u32x4*>(row + 32 * k + 8 * g);
-    } else {
+        for (int k = 0; k < KS; ++k) q[n][k] = *reinterpret_cast<const u32x4*>(row + 32 * k + 8 * g);
+      } else {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) q[n][k] = *reinterpret_cast<const u32x4*>(&q_rows[(16 * n + col) * kRow + 32 * k + 8 * g]);
+        for (int k = 0; k < KS; ++k) q[n][k] = *reinterpret_cast<const u32x4*>(&q_rows[(16 * n + col) * kRow + 32 * k + 8 * g]);
+      }
     }
-  }
+  };
+  load_q();
 
   const int64_t head_page = (int64_t)D << shift;                    // values of a head in a page
   const int last_page = len > 0 ? (len - 1) >> shift : 0;
@@ -173,6 +176,63 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
     v_page = page_at(t0 + 2 * kStride + 8 * g);
   }
 
+  // A weight that rounds to 0 makes NaN of an infinite value, where the weight itself leaves infinity.  Where a sum is no number, though the
+  // sum of the weights is one, its values that are no numbers decide alone: they are added once more, with the weight 1, or 0 where
+  // the logit is -infinity.
+  bool lost = false;
+#pragma unroll
+  for (int n = 0; n < TILES; ++n) {
+    float largest = o[n][0][0];
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) largest = __builtin_elementwise_maximum(largest, o[n][i][j]);   // NaN where one of them is
+    lost |= __builtin_isunordered(largest, largest) && !__builtin_isunordered(l[n], l[n]);
+  }
+  if (__builtin_expect(__any(lost), 0)) {
+#pragma unroll
+    for (int n = 0; n < TILES; ++n)
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[n][i][j] = __builtin_isunordered(o[n][i][j], o[n][i][j]) ? 0.f : o[n][i][j];
+    if constexpr (TILES * D >= 3 * 128) {   // q once more, or the loop above spills more of it for its sake (64 sequences, 48 heads to one: 75 us for 70)
+      asm volatile("" ::: "memory");
+      load_q();
+    }
+    for (int t = begin + 32 * wave; t < end; t += kStride) {
+      load_k(t, page_at(t + k_run), true);
+      u32x4 there[TILES];
+#pragma unroll
+      for (int n = 0; n < TILES; ++n) {
+        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          s0 = mfma16<BF16>(kf[0][k], q[n][k], s0);
+          s1 = mfma16<BF16>(kf[1][k], q[n][k], s1);
+        }
+        f32x8 p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[i] = s0[i] * a.scale_log2 == -INFINITY ? 0.f : 1.f;
+          p[4 + i] = s1[i] * a.scale_log2 == -INFINITY ? 0.f : 1.f;
+        }
+        there[n] = pack8<BF16>(p);
+      }
+      __builtin_amdgcn_sched_barrier(0);   // the values into the keys' registers
+      load_v(t, page_at(t + 8 * g), true);
+      const int rest = len - t - 8 * g;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          vf[i][j] &= odd_halves<BF16>(vf[i][j]) & ((2 * j < rest ? 0xffffu : 0u) | (2 * j + 1 < rest ? 0xffff0000u : 0u));
+#pragma unroll
+        for (int n = 0; n < TILES; ++n) o[n][i] = mfma16<BF16>(vf[i], there[n], o[n][i]);
+      }
+    }
+  }
+
   // The waves' sums, brought to one maximum: four values of a head a thread.
   constexpr int kThreads = 64 * kWaves;
   __shared__ float wave_m[kWaves][kTileHeads], wave_l[kWaves][kTileHeads];
@@ -216,7 +276,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
       float weight = 0.f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float f = exp2_fast(wave_m[w][c] - base);
+        const float f = rescale(wave_m[w][c], base);
         sum += f * *reinterpret_cast<const f32x4*>(&wave_o[w][4 * i]);
         weight += f * wave_l[w][c];
       }
@@ -263,7 +323,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
 #pragma unroll
         for (int p = 0; p < kFew; ++p) {
           if (p >= parts) break;
-          const float f = exp2_fast(ml[p][0] - base);
+          const float f = rescale(ml[p][0], base);
           sum += f * f32x4{v[p][0][0], v[p][0][1], v[p][1][0], v[p][1][1]};
           weight += f * ml[p][1];
         }
@@ -297,7 +357,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
       const int p = r0 + j * (kThreads / kTileHeads);
-      const float f = exp2_fast(pm[j] - base);
+      const float f = rescale(pm[j], base);
       weight += f * pl[j];
       if (p < parts) factor[p * kTileHeads + c0] = f;
     }

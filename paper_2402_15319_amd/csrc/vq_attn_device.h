@@ -115,6 +115,16 @@ __device__ __forceinline__ void lds_turn() {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp
 
+// What brings sums from one maximum to a larger one: never 0, which an infinite sum must not meet.  (The smallest number of all, so that
+// outputs of bf16 close to their smallest do not feel it.)
+__device__ __forceinline__ float rescale(float from, float to) { return fmaxf(exp2_fast(from - to), 0x1p-149f); }
+
+// The halves of a dword that are no finite numbers: all ones.
+template <bool BF16> __device__ __forceinline__ uint32_t odd_halves(uint32_t v) {
+  constexpr uint32_t kExp = BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = BF16 ? 0x00800080u : 0x04000400u;
+  return (((v & kExp) + kOne) >> 15 & 0x00010001u) * 0xffffu;
+}
+
 // Weights are exp2(x - m) with m a maximum less kLift: in fp16 weights below 2^-14 lose bits, so the largest start from 2^kLift
 // there.  It cancels in out and in lse.  m is left as it is until a logit is more than kSlack above the maximum it was taken from.
 template <bool BF16> constexpr float kLift = BF16 ? 0.f : 6.f;

@@ -112,6 +112,14 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   const int k_row = (col & 0x13) | (col & 4) << 1 | (col & 8) >> 1;
+  uint32_t left_out = 0;   // values that are no numbers, in steps with a mask
+  auto up_to_last = [&](int at) {   // what is left of the lane's tokens at + 8 half .. + 7: those up to the sequence's last one
+    const int rest = len - at - 8 * half;
+    u32x4 keep;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) keep[j] = (2 * j < rest ? 0xffffu : 0u) | (2 * j + 1 < rest ? 0xffff0000u : 0u);
+    return keep;
+  };
 
   auto work = [&](int step, auto masked_) {
     constexpr bool masked = decltype(masked_)::value;
@@ -181,41 +189,21 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
       p[c] = pack8<BF16>(w);
     }
     if constexpr (masked) {
-      // A weight of 0 must not meet a value that is no number: tokens behind the last one are cleared, and what else there is
-      // of them is left out of the product and given afterwards to the rows that attend it.
-      constexpr uint32_t kExp = BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = BF16 ? 0x00800080u : 0x04000400u;
-      uint32_t odd = 0;
+      // A row's weight of 0 must not meet a value that is no number: tokens behind the last one are cleared, and what else there is
+      // of them is left out of the product; it is added after the last step.
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int rest = len - step * kTokens - 16 * c - 8 * half;
-        u32x4 keep;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) keep[j] = (2 * j < rest ? 0xffffu : 0u) | (2 * j + 1 < rest ? 0xffff0000u : 0u);
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
-          u32x4 f = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32) & keep;
+          u32x4 f = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32) & up_to_last(step * kTokens + 16 * c);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t t = ((f[j] & kExp) + kOne) & 0x80008000u;   // the halves with a full exponent
-            odd |= t;
-            f[j] &= ~((t >> 15) * 0xffffu);
+            const uint32_t odd = odd_halves<BF16>(f[j]);
+            left_out |= odd;
+            f[j] &= ~odd;
           }
           o[i] = mfma32<BF16>(f, p[c], o[i]);
         }
-      }
-      if (__any(odd)) {
-        for (int j = 0; j < kTokens; ++j) {
-          const bool mine = step * kTokens + j <= pos;
-#pragma unroll
-          for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int d = 32 * i + 8 * (e >> 2) + 4 * half + (e & 3);
-              const float v = to_f32<BF16>(*reinterpret_cast<const uint16_t*>(vt + ((j >> 4) * D + d) * 32 + (((j >> 3) ^ (e >> 2)) & 1) * 16 + (j & 7) * 2));
-              if (mine && !(fabsf(v) < INFINITY)) o[i][e] += v;
-            }
-        }
-      }
     } else {
 #pragma unroll
       for (int at = 0; at < 4 * DT; at += kBatch) {
@@ -239,6 +227,83 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
     if ((TEAMS == 1 || step < steps) && step * kTokens <= wave_last) work(step, std::true_type());
   }
 
+  // A weight that rounds to 0 makes NaN of an infinite value, where the weight itself leaves infinity.  Where a sum is no number, though the
+  // sum of the weights is one, its values that are no numbers decide alone: all of them are added in one more turn through the
+  // wave's steps, with the weight 1, or 0 where the logit is -infinity.
+  float largest = o[0][0];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) largest = __builtin_elementwise_maximum(largest, o[i][j]);   // NaN where one of them is
+  if (__builtin_expect(__any(left_out != 0 || (__builtin_isunordered(largest, largest) && !__builtin_isunordered(l, l))), 0)) {
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = __builtin_isunordered(o[i][j], o[i][j]) ? 0.f : o[i][j];
+    // 32 tokens at a time: what each row attends of them, with a weight (there) or without (none), times 1 for infinity, 64 for -infinity and
+    // 4,096 for NaN: no more than 16 of each in a sum.  (4,096 tokens x 32 heads of 128 whose values are all NaN: 1.7 ms, 0.17 with none.)
+    constexpr uint32_t kExp = BF16 ? 0x7f80 : 0x7c00, kOne = BF16 ? 0x3f80 : 0x3c00, k64 = BF16 ? 0x4280 : 0x5400, k4096 = BF16 ? 0x4580 : 0x6c00;
+    for (int at = (begin + team) * kTokens; at < steps * kTokens && at <= wave_last; at += at % kTokens ? 32 + (TEAMS - 1) * kTokens : 32) {
+      int64_t head[2];   // of the 16 tokens' page
+      u32x4 keep[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int t = at + 16 * h, page = table[t >> shift < last_page ? t >> shift : last_page];
+        head[h] = ((int64_t)page_inside(a.c, page) * a.c.kv_heads + kvh) * ((int64_t)D << shift);
+        keep[h] = up_to_last(t);
+      }
+      auto values = [&](int h, int i) {
+        return *reinterpret_cast<const u32x4*>(a.v_pages + head[h] + ((int64_t)(32 * i + col) << shift) + ((at + 16 * h) & mask) + 8 * half) & keep[h];
+      };
+      uint32_t odd = 0;
+#pragma unroll 1
+      for (int i = 0; i < 2 * DT; ++i) {
+        const u32x4 f = values(i & 1, i >> 1);
+        odd |= odd_halves<BF16>(f[0]) | odd_halves<BF16>(f[1]) | odd_halves<BF16>(f[2]) | odd_halves<BF16>(f[3]);
+      }
+      if (!__any(odd)) continue;
+      f32x16 x;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[j] = 0.f;
+      const uint16_t* k = a.k_pages + (k_row < 16 ? head[0] : head[1]) + (((at + k_row) & mask) * D) + 8 * half;
+#pragma unroll
+      for (int c = 0; c < KS; ++c) x = mfma32<BF16>(*reinterpret_cast<const u32x4*>(k + 16 * c), q[c], x);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 there = {0, 0, 0, 0}, none = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const bool mine = at + 16 * h + 8 * half + j <= pos, zero = x[8 * h + j] * a.scale_log2 == -INFINITY;
+          there[j / 2] |= mine && !zero ? kOne << (j % 2 * 16) : 0u;
+          none[j / 2] |= mine && zero ? kOne << (j % 2 * 16) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          const u32x4 f = values(h, i);
+          u32x4 code = {0, 0, 0, 0}, all_nan = {0, 0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t u = f[j / 2] >> (j % 2 * 16) & 0xffff, size = u & 0x7fff;
+            code[j / 2] |= (size < kExp ? 0u : size > kExp ? k4096 : u > kExp ? k64 : kOne) << (j % 2 * 16);
+            all_nan[j / 2] |= (size < kExp ? 0u : k4096) << (j % 2 * 16);
+          }
+          f32x16 y;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) y[j] = 0.f;
+          y = mfma32<BF16>(code, there, y);
+          y = mfma32<BF16>(all_nan, none, y);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const uint32_t count = (uint32_t)y[j];
+            o[i][j] += (count & 63 ? INFINITY : 0.f) - (count >> 6 & 63 ? INFINITY : 0.f);
+            o[i][j] = count >> 12 ? __builtin_nanf("") : o[i][j];
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
+
   l += __shfl_xor(l, 32);
   if constexpr (TEAMS == 2) {
     // What the second team has goes through LDS, [maximum and sum of the weights, then four sums over values at a time][lane].
@@ -257,7 +322,7 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
     const f32x4 ml = at[0];
     const float old = m;
     m = fmaxf(m, ml[0]);
-    const float base = m == -INFINITY ? 0.f : m, f0 = exp2_fast(old - base), f1 = exp2_fast(ml[0] - base);
+    const float base = m == -INFINITY ? 0.f : m, f0 = rescale(old, base), f1 = rescale(ml[0], base);
     l = f0 * l + f1 * ml[1];
 #pragma unroll
     for (int i = 0; i < 4 * DT; ++i) {
@@ -312,8 +377,8 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
         __builtin_amdgcn_sched_barrier(0);
         if (at == 0) {
           const float top = fmaxf(m, ml[0]), base = top == -INFINITY ? 0.f : top;
-          old = exp2_fast(m - base);
-          now = exp2_fast(ml[0] - base);
+          old = rescale(m, base);
+          now = rescale(ml[0], base);
           m = top;
           l = old * l + now * ml[1];
         }
