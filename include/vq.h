@@ -311,7 +311,8 @@ typedef struct vq_attn_batch {
                                  n_tokens * heads / 128 + n_seqs * heads is at most 2^20             */
   int32_t table_width;        /* pages that a row of page_table lists, >= 1                          */
   int32_t max_len;            /* no kv_len is larger; [0, table_width * page_size], at most 2^29.
-                                 Decides how the work is split; a larger kv_len is taken as max_len  */
+                                 Decides how the work is split.  Attention takes a larger kv_len as
+                                 max_len; new tokens at positions from max_len on are not written    */
   const int32_t* q_start;     /* [n_seqs + 1], ascending from 0 to n_tokens; NULL: one new token for
                                  each sequence (n_tokens = n_seqs)                                   */
   const int32_t* kv_len;      /* [n_seqs]                                                            */
@@ -330,8 +331,8 @@ VQ_API int vq_cache_bytes(const vq_attn_desc* desc, size_t* bytes);
 
 /*
  * The new tokens' keys and values into their pages, copied bit for bit; k and v are
- * [n_tokens][kv_heads][head_dim] with the strides given.  Tokens with a negative position, or in
- * a page outside the cache, are left out.  k, v, k_pages and v_pages are 16-byte aligned and do not
+ * [n_tokens][kv_heads][head_dim] with the strides given.  Tokens with a negative position, with one
+ * of max_len or more, or in a page outside the cache, are left out.  k, v, k_pages and v_pages are 16-byte aligned and do not
  * overlap.  desc->scale is not used.  One launch.
  */
 VQ_API int vq_cache_append(const vq_attn_desc* desc, const vq_attn_batch* batch,

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void 
   const int part = blockIdx.z, s = blockIdx.y;
   const int beside = (A.plan.tiles + TILES - 1) / TILES, kvh = blockIdx.x / beside, tile0 = (blockIdx.x - kvh * beside) * TILES;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
-  const int len = cached_tokens(a.c, s);
+  const int len = cached_tokens(a.c, s, a.c.max_len);
   const int begin = part * A.plan.chunk;
   if (begin >= len && part > 0) return;
   const int end = len - begin < A.plan.chunk ? len : begin + A.plan.chunk;

@@ -14,24 +14,28 @@ template <bool BF16> __device__ __forceinline__ uint16_t from_f32(float f) {
   else return __builtin_bit_cast(uint16_t, (_Float16)f);
 }
 
-// Tokens in the cache of sequence s: what the table can list at most.
-__device__ __forceinline__ int cached_tokens(const CacheArgs& c, int s) {
+// Tokens in the cache of sequence s: `most` at most.
+__device__ __forceinline__ int cached_tokens(const CacheArgs& c, int s, int most) {
   const int n = c.kv_len[s];
-  return n < 0 ? 0 : n < c.max_len ? n : c.max_len;
+  return n < 0 ? 0 : n < most ? n : most;
 }
+// Attention takes a longer sequence as one of max_len tokens.  New tokens keep their positions, and those from max_len on have no place; with
+// 2^30 for more than that, none of them has one (max_len is at most 2^29, there are little more than 2^27 new tokens at most) and no
+// index overflows.
+constexpr int kFarBeyond = 1 << 30;
 
 // Work is handed out in tiles of `unit` new tokens of a sequence, at most floor(tokens / unit) + extra of them.  Those of
 // sequence i start at slot floor(first token / unit) + extra * i, which leaves room for the last ones of the sequences before;
 // this is the sequence of a slot, the slot's number among its own, the sequence's rows (new tokens) first .. last - 1 and the tokens
-// in its cache, all inside the arrays whatever they hold.  A wave looks at 64 sequences at a time, with one wait for all of it.
+// in its cache (`most` at most), all inside the arrays whatever they hold.  A wave looks at 64 sequences at a time, with one wait for all of it.
 struct Tile { int sequence, number, first, last, cached; };
-__device__ __forceinline__ Tile tile_of(const CacheArgs& c, int slot, int unit, int extra) {
+__device__ __forceinline__ Tile tile_of(const CacheArgs& c, int slot, int unit, int extra, int most) {
   const int lane = threadIdx.x & 63;
   Tile t = {0, slot, 0, 0, 0};   // an empty sequence, where q_start does not begin with 0
   for (int base = 0; base < c.n_seqs; base += 64) {
     const int i = base + lane, in = i < c.n_seqs ? i : c.n_seqs - 1;
     int first = c.q_start ? c.q_start[in] : in, last = c.q_start ? c.q_start[in + 1] : in + 1;
-    const int cached = cached_tokens(c, in);
+    const int cached = cached_tokens(c, in, most);
     first = first < 0 ? 0 : first < c.n_tokens ? first : c.n_tokens;
     last = last < first ? first : last < c.n_tokens ? last : c.n_tokens;
     const int at = first / unit + extra * i;

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
   const int group = a.group, heads_in = A.plan.heads, wide = a.heads / heads_in;   // query heads of a tile; tiles beside one another
   const int slot = (int)A.plan.slots - 1 - blockIdx.x / wide, beside = blockIdx.x % wide, head0 = beside * heads_in, kvh = head0 / group;
   const int tokens = A.plan.tokens;
-  const Tile tile = tile_of(a.c, slot, tokens, 1);
+  const Tile tile = tile_of(a.c, slot, tokens, 1, a.c.max_len);
   const int s = tile.sequence, first = tile.first, n = tile.last - first, len = tile.cached, behind = len - n;   // new token i: position behind + i
   const int token0 = tile.number * tokens;
   if (token0 >= n) return;

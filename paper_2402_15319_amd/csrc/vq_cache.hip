@@ -28,9 +28,9 @@ __device__ __forceinline__ int64_t head_of(const CacheArgs& c, int s, int pos, i
 // A token at a time: a thread takes eight dimensions of a head's key and value.
 __global__ __launch_bounds__(256) void append_one_kernel(const AppendArgs a, int head_dim) {
   const int t = blockIdx.x, pieces = head_dim / 8, i = blockIdx.y * 256 + threadIdx.x, h = i / pieces, d = 8 * (i - h * pieces);
-  const Tile tile = a.c.q_start ? tile_of(a.c, t, 1, 0) : Tile{t, 0, t, t + 1, cached_tokens(a.c, t)};
+  const Tile tile = a.c.q_start ? tile_of(a.c, t, 1, 0, kFarBeyond) : Tile{t, 0, t, t + 1, cached_tokens(a.c, t, kFarBeyond)};
   const int s = tile.sequence, pos = tile.cached - tile.last + t;
-  if (h >= a.c.kv_heads || t < tile.first || t >= tile.last || pos < 0) return;
+  if (h >= a.c.kv_heads || t < tile.first || t >= tile.last || pos < 0 || pos >= a.c.max_len) return;
   const int size = 1 << a.c.page_shift, slot = pos & (size - 1);
   const uint16_t* k = a.k + t * a.ks.token + h * a.ks.head + d * a.ks.dim;
   const uint16_t* v = a.v + t * a.vs.token + h * a.vs.head + d * a.vs.dim;
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const App
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool values = wave >= kHalves;
   const int h = blockIdx.x % a.c.kv_heads;
-  const Tile tile = tile_of(a.c, blockIdx.x / a.c.kv_heads, kTile, 2);
+  const Tile tile = tile_of(a.c, blockIdx.x / a.c.kv_heads, kTile, 2, kFarBeyond);
   const int s = tile.sequence, first = tile.first, last = tile.last;
   const int behind = tile.cached - last, from = behind + first > 0 ? behind + first : 0;   // token t has position behind + t
   // lanes: positions first where the source runs along them, dimensions first where it runs along those
@@ -64,7 +64,8 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append_kernel(const App
   const bool spread = D % 64 == 0 && values && along_tokens;
   const int d = 64 * (wave % kHalves) + (spread ? y : 8 * y), d_step = spread ? 8 : 1;
   const int64_t dim = st.dim * d_step;
-  const int lo = from - pos > 0 ? from - pos : 0, end = behind + last - pos, hi = end < 8 ? end : 8;   // its positions lo .. hi - 1 are new
+  const int stop = tile.cached < a.c.max_len ? tile.cached : a.c.max_len;
+  const int lo = from - pos > 0 ? from - pos : 0, hi = stop - pos < 8 ? stop - pos : 8;   // its positions lo .. hi - 1 are new and have a place
   if (lo >= hi || d >= D) return;
   const int64_t base = head_of(a.c, s, pos, h, D);
   if (base < 0) return;
