@@ -73,9 +73,13 @@ def generate(block: AttentionBlock, prompts, steps: int, continuations: int, pag
     per = -(-longest // page_size)
     cache = PagedCache(1, block.heads, block.kv_heads, block.head_dim, page_size, per * (len(prompts) + continuations), per)
     seqs, new = [cache.add() for _ in prompts], [p.shape[1] for p in prompts]
+    users = len(prompts) + max(0, continuations - 1)
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=DEV)  # noqa: E731
+    largest = vq.AttnBatch(ints(users), ints(users, per), n_tokens=max(sum(new), users), max_len=longest, q_start=ints(users + 1))
+    workspace = vq.attn_workspace(cache.desc, largest, DEV)   # serves every smaller batch
     cache.grow(seqs, new)
     batch = cache.batch(seqs, new)
-    y = block(columns(torch.cat(list(prompts), dim=1)), cache, 0, batch, vq.attn_workspace(cache.desc, batch), prompt=True)
+    y = block(columns(torch.cat(list(prompts), dim=1)), cache, 0, batch, workspace, prompt=True)
     outputs = [[part] for part in y.split(new, dim=1)]
     for _ in range(continuations - 1):
         seqs.append(cache.fork(seqs[0]))
@@ -87,7 +91,7 @@ def generate(block: AttentionBlock, prompts, steps: int, continuations: int, pag
         # a real decoder goes on from a sampled token's embedding; here each sequence goes its way by some noise
         x = torch.stack([o[-1][:, -1] for o in outputs], dim=1)
         x = 0.5 * x + 0.5 * torch.randn(x.shape, device=DEV, dtype=x.dtype, generator=gen)
-        y = block(columns(x), cache, 0, batch, vq.attn_workspace(cache.desc, batch), prompt=False)
+        y = block(columns(x), cache, 0, batch, workspace, prompt=False)
         for i, o in enumerate(outputs):
             o.append(y[:, i:i + 1])
     if len(seqs) > 2:       # a user leaves; what remains moves together

@@ -353,7 +353,8 @@ VQ_API int vq_cache_copy(const vq_attn_desc* desc, int n_buffers, void* const* b
 
 /*
  * Bytes of the workspace that vq_attn_decode and vq_attn_prompt need for a batch of these sizes
- * (host fields of `batch` only; at least 16).  The workspace is device memory owned by the caller,
+ * (host fields of `batch` only; at least 16), and for every batch of no more sequences, new tokens and
+ * tokens in a sequence (max_len) with the same descriptor: a program that asks for its largest needs no other.  The workspace is device memory owned by the caller,
  * 16-byte aligned, and all zero before its first use; every call leaves it fit for the next.  Calls
  * that share a workspace must not overlap in time.
  */

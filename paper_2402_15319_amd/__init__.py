@@ -382,7 +382,8 @@ def vq_attn_workspace_bytes(desc: VQAttnDesc, batch: AttnBatch) -> int:
 
 
 def attn_workspace(desc: VQAttnDesc, batch: AttnBatch, device="cuda:0"):
-    """A workspace for vq_attn_decode and vq_attn_prompt, ready for use."""
+    """A workspace for vq_attn_decode and vq_attn_prompt, ready for use: for this batch and every one of no more sequences, new tokens
+    and max_len."""
     import torch
     return torch.zeros(vq_attn_workspace_bytes(desc, batch), dtype=torch.uint8, device=device)
 

@@ -128,6 +128,7 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
 }
 
 constexpr int kLeastSteps = 8;          // of a part
+constexpr int64_t kOneTeamUnits = 512, kWideUnits = 448;   // workgroups that the chip runs at once, or nearly: of one team, and of heads of 256
 
 PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   PromptPlan p;
@@ -159,7 +160,7 @@ PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   p.teams = d.head_dim <= 128 && (lone || few) ? 2 : 1;
   // Parts, where they bring the workgroups near to what the chip runs at once (heads of 256 have one workgroup to a compute unit, and of
   // longer parts: 16 heads, 1,500 and 2,048 tokens 67 and 88 us whole, 51 and 80 in two parts).
-  const int64_t enough = p.teams == 2 ? 256 : d.head_dim > 128 ? 448 : 512;
+  const int64_t enough = p.teams == 2 ? kEnoughUnits : d.head_dim > 128 ? kWideUnits : kOneTeamUnits;
   int64_t parts = units < enough ? (enough + units / 2) / units : 1;
   while (parts > 1 && parts * parts > steps) --parts;   // to join a part takes about as long as a step
   int64_t per = (steps + parts - 1) / parts;
@@ -169,16 +170,52 @@ PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   return p;
 }
 
-// Bytes of the workspace: the counters and what the parts leave, where there are several.
-size_t decode_workspace(const vq_attn_desc& d, const vq_attn_batch& b) {
+// The most parts that vq_attn_decode leaves in all tiles together, over batches of no more than n_seqs sequences of up to max_len tokens: those
+// of decode_plan above, with the tiles and the units that such a batch has at most.
+int64_t decode_most_parts(const vq_attn_desc& d, int64_t n_seqs, int64_t max_len) {
+  if (max_len * d.head_dim <= kShortValues) return 0;
+  vq_attn_batch b = {};
+  b.n_seqs = b.n_tokens = 65535;   // enough for several tiles to a workgroup, where there are several
+  b.max_len = 1;
   const DecodePlan p = decode_plan(d, b);
-  if (p.parts <= 1) return 16;
-  return kJoinCounters * sizeof(uint32_t) + (size_t)b.n_seqs * d.kv_heads * p.tiles * p.parts * part_floats(p, d.head_dim) * sizeof(float);
+  const auto least = [](int64_t tokens) { return tokens < 1 ? 1 : tokens; };
+  const int64_t steps = (max_len + kPartStep - 1) / kPartStep, most = steps < kMostParts ? steps : kMostParts;
+  const int64_t wide = d.kv_heads * (int64_t)((p.tiles + p.together - 1) / p.together), tiles = n_seqs * d.kv_heads * p.tiles;
+  // Fewer than kEnoughUnits units: parts of kLongPart tokens, and up to kEnoughUnits / units - 1 more for as many on every CU.
+  const int64_t few = tiles < (kEnoughUnits - 1) * p.together ? tiles : (kEnoughUnits - 1) * p.together;
+  const int64_t by_length = few * least((steps * kPartStep + kLongPart - 1) / kLongPart) + (kEnoughUnits - 1) * p.together;
+  int64_t parts = few * most < by_length ? few * most : by_length;
+  if (n_seqs * wide >= kEnoughUnits) {
+    const int64_t many = tiles < kJoinCounters ? tiles : kJoinCounters, each = least((steps * kPartStep + kShortPart - 1) / kShortPart);
+    const int64_t of_many = many * (each < most ? each : most);
+    parts = of_many > parts ? of_many : parts;
+  }
+  return parts;
 }
-size_t prompt_workspace(const vq_attn_desc& d, const vq_attn_batch& b) {
-  const PromptPlan p = prompt_plan(d, b);
-  if (p.parts <= 1) return 16;
-  return kJoinCounters * sizeof(uint32_t) + (size_t)p.slots * (d.heads / p.heads) * p.parts * prompt_part_floats(d.head_dim) * sizeof(float);
+
+// The same of vq_attn_prompt: a call has parts where its units are fewer than `enough`, and then up to enough + units / 2 of them; its
+// units are at most those of tiles of 64 rows and two tiles of one row's heads for each sequence.
+int64_t prompt_most_parts(const vq_attn_desc& d, int64_t n_seqs, int64_t n_tokens, int64_t max_len) {
+  const int64_t steps = (max_len + kPromptTokens - 1) / kPromptTokens, enough = d.head_dim > 128 ? kWideUnits : kOneTeamUnits;
+  const int64_t of_steps = (steps + kLeastSteps - 1) / kLeastSteps, of_join = (int64_t)sqrt((double)steps);   // steps below 2^24: exact
+  const int64_t each = of_steps < of_join ? of_steps : of_join;
+  if (each <= 1) return 0;
+  int64_t units = n_tokens * d.heads / 64 + 2 * n_seqs * d.heads;
+  units = units < enough ? units : enough;
+  const int64_t all = enough + enough / 2;
+  return units * each < all ? units * each : all;
+}
+
+// Bytes of the workspace: the counters and what the parts leave, for this batch and every one of no more sequences, new tokens and
+// tokens in a sequence.  (What a batch itself needs does not grow with it: fewer workgroups are split into more parts.)
+size_t workspace(const vq_attn_desc& d, const vq_attn_batch& b) {
+  const int64_t decode = decode_most_parts(d, b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens, b.max_len);
+  const int64_t prompt = prompt_most_parts(d, b.n_seqs, b.n_tokens, b.max_len);
+  if (decode == 0 && prompt == 0) return 16;
+  DecodePlan tile = {};
+  tile.cols = d.heads / d.kv_heads < kTileHeads ? d.heads / d.kv_heads : kTileHeads;
+  const size_t of_decode = (size_t)decode * part_floats(tile, d.head_dim), of_prompt = (size_t)prompt * prompt_part_floats(d.head_dim);
+  return (kJoinCounters + (of_decode > of_prompt ? of_decode : of_prompt)) * sizeof(float);
 }
 
 int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,
@@ -197,7 +234,7 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   if (st != VQ_OK) return st;
   st = check_strides(out_strides, batch->n_tokens, desc->heads, desc->head_dim, true, &a.os);
   if (st != VQ_OK) return st;
-  if (workspace_bytes < (decode ? decode_workspace(*desc, *batch) : prompt_workspace(*desc, *batch))) return VQ_ERR_BAD_ARG;
+  if (workspace_bytes < vq::workspace(*desc, *batch)) return VQ_ERR_BAD_ARG;
   a.c = cache_args(*desc, *batch, decode);
   a.q = (const uint16_t*)q;
   a.k_pages = (const uint16_t*)k_pages;
@@ -315,8 +352,7 @@ int vq_attn_workspace_bytes(const vq_attn_desc* desc, const vq_attn_batch* batch
   st = check_batch_sizes(*desc, batch);
   if (st != VQ_OK) return st;
   if (!bytes) return VQ_ERR_NULL;
-  const size_t prompt = prompt_workspace(*desc, *batch), decode = batch->n_tokens == batch->n_seqs ? decode_workspace(*desc, *batch) : 0;
-  *bytes = prompt > decode ? prompt : decode;
+  *bytes = vq::workspace(*desc, *batch);
   return VQ_OK;
 }
 
