@@ -323,12 +323,16 @@ class AttnBatch:
 
     def __init__(self, kv_len, page_table, n_tokens: int | None = None, max_len: int | None = None, q_start=None, page_size: int | None = None):
         import torch
+        _kinds.update({VQ_F16: torch.float16, VQ_BF16: torch.bfloat16, VQ_F32: torch.float32})
         for what, t, dim in (("kv_len", kv_len, 1), ("page_table", page_table, 2), ("q_start", q_start, 1)):
             if t is not None and (t.dtype != torch.int32 or t.dim() != dim or not t.is_contiguous()):
                 raise ValueError(f"AttnBatch: {what} is a contiguous int32 tensor of {dim} dimension(s)")
         n = kv_len.shape[0]
         if page_table.shape[0] != n or (q_start is not None and q_start.shape[0] != n + 1):
             raise ValueError("AttnBatch: arrays of different numbers of sequences")
+        self.gpu = kv_len.get_device()   # -1: on the host, which is enough for sizes
+        if page_table.get_device() != self.gpu or (q_start is not None and q_start.get_device() != self.gpu):
+            raise ValueError("AttnBatch: arrays on different devices")
         if n_tokens is None:
             if q_start is not None:
                 raise ValueError("AttnBatch: n_tokens is needed with q_start")
@@ -342,11 +346,26 @@ class AttnBatch:
         self._keep = (kv_len, page_table, q_start)
 
 
-def _rows(t, n: int, heads: int, dim: int, what: str):
+_kinds: dict = {}   # VQ_F16, VQ_BF16, VQ_F32: the torch type (filled by the first AttnBatch)
+
+
+def _rows(t, n: int, heads: int, dim: int, what: str, kind, gpu: int):
     """The strides of a [n, heads, dim] tensor; None where it has no gaps."""
-    if t.shape != (n, heads, dim) or t.element_size() != 2:
-        raise ValueError(f"{what}: a 16-bit tensor [{n}, {heads}, {dim}] is wanted, not {t.dtype} {tuple(t.shape)}")
+    if t.shape != (n, heads, dim) or t.dtype is not kind or t.get_device() != gpu or gpu < 0:
+        raise ValueError(f"{what}: a tensor [{n}, {heads}, {dim}] of the descriptor's type on the GPU of the batch's arrays is wanted, not {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
     return None if t.is_contiguous() else VQStrides(*t.stride())
+
+
+def _pages(t, size: int, what: str, kind, gpu: int) -> int:
+    """The address of a K or V buffer (an address passes through)."""
+    try:
+        if t.dtype is kind and t.nbytes >= size and t.get_device() == gpu and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        return _ptr(t)
+    raise ValueError(f"{what}: a contiguous tensor of the descriptor's type and of {size} bytes or more on the batch's GPU is wanted, not {t.dtype} "
+                     f"{tuple(t.shape)} on {t.device}")
 
 
 def vq_cache_bytes(desc: VQAttnDesc) -> int:
@@ -357,13 +376,16 @@ def vq_cache_bytes(desc: VQAttnDesc) -> int:
 
 def vq_cache_append(desc: VQAttnDesc, batch: AttnBatch, k, v, k_pages, v_pages, stream=None) -> None:
     """k, v: [n_tokens, kv_heads, head_dim] views (strides as vq_strides allows) of the new tokens."""
-    n, heads, dim = batch.n_tokens, desc.kv_heads, desc.head_dim
-    _check(lib().vq_cache_append(desc, batch.struct, k.data_ptr(), _rows(k, n, heads, dim, "k"), v.data_ptr(), _rows(v, n, heads, dim, "v"),
-                                 _ptr(k_pages), _ptr(v_pages), _stream(stream)), "vq_cache_append")
+    n, heads, dim, kind, gpu = batch.n_tokens, desc.kv_heads, desc.head_dim, _kinds.get(desc.dtype), batch.gpu
+    size = 2 * desc.n_pages * heads * desc.page_size * dim
+    _check(lib().vq_cache_append(desc, batch.struct, k.data_ptr(), _rows(k, n, heads, dim, "k", kind, gpu), v.data_ptr(),
+                                 _rows(v, n, heads, dim, "v", kind, gpu), _pages(k_pages, size, "k_pages", kind, gpu),
+                                 _pages(v_pages, size, "v_pages", kind, gpu), _stream(stream)), "vq_cache_append")
 
 
 def vq_cache_copy(desc: VQAttnDesc, buffers, from_to, stream=None) -> None:
-    """buffers: K and V buffers; from_to: (page, page) pairs, copied one after another in every buffer."""
+    """buffers: K and V buffers, whole ones (vq_cache_bytes each, on the current GPU: of so many this is not checked); from_to: (page,
+    page) pairs, copied one after another in every buffer."""
     try:
         flat = array.array("i", [p for a, b in from_to for p in (a, b)])
     except (ValueError, TypeError, OverflowError) as e:
@@ -389,11 +411,15 @@ def attn_workspace(desc: VQAttnDesc, batch: AttnBatch, device="cuda:0"):
 
 
 def _attn(call, name, desc, batch, q, k_pages, v_pages, out, workspace, lse, stream):
-    n, heads, dim = batch.n_tokens, desc.heads, desc.head_dim
-    if lse is not None and (lse.shape != (n, heads) or lse.element_size() != 4 or not lse.is_contiguous()):
-        raise ValueError(f"{name}: lse is a contiguous float32 tensor [n_tokens, heads]")
-    _check(call(desc, batch.struct, q.data_ptr(), _rows(q, n, heads, dim, "q"), _ptr(k_pages), _ptr(v_pages), out.data_ptr(),
-                _rows(out, n, heads, dim, "out"), _ptr(lse), _ptr(workspace), workspace.nbytes, _stream(stream)), name)
+    n, heads, dim, kind, gpu = batch.n_tokens, desc.heads, desc.head_dim, _kinds.get(desc.dtype), batch.gpu
+    size = 2 * desc.n_pages * desc.kv_heads * desc.page_size * dim
+    if lse is not None and (lse.shape != (n, heads) or lse.dtype is not _kinds[VQ_F32] or not lse.is_contiguous() or lse.get_device() != gpu):
+        raise ValueError(f"{name}: lse is a contiguous float32 tensor [n_tokens, heads] on the batch's GPU")
+    if workspace.get_device() != gpu:
+        raise ValueError(f"{name}: the workspace is on the batch's GPU")
+    _check(call(desc, batch.struct, q.data_ptr(), _rows(q, n, heads, dim, "q", kind, gpu), _pages(k_pages, size, "k_pages", kind, gpu),
+                _pages(v_pages, size, "v_pages", kind, gpu), out.data_ptr(), _rows(out, n, heads, dim, "out", kind, gpu), _ptr(lse),
+                _ptr(workspace), workspace.nbytes, _stream(stream)), name)
 
 
 def vq_attn_decode(desc: VQAttnDesc, batch: AttnBatch, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:
