@@ -330,7 +330,7 @@ class AttnBatch:
         n = kv_len.shape[0]
         if page_table.shape[0] != n or (q_start is not None and q_start.shape[0] != n + 1):
             raise ValueError("AttnBatch: arrays of different numbers of sequences")
-        self.gpu = kv_len.get_device()   # -1: on the host, which is enough for sizes
+        self.device, self.gpu = kv_len.device, kv_len.get_device()   # -1: on the host, which is enough for sizes
         if page_table.get_device() != self.gpu or (q_start is not None and q_start.get_device() != self.gpu):
             raise ValueError("AttnBatch: arrays on different devices")
         if n_tokens is None:
@@ -403,11 +403,11 @@ def vq_attn_workspace_bytes(desc: VQAttnDesc, batch: AttnBatch) -> int:
     return a.value
 
 
-def attn_workspace(desc: VQAttnDesc, batch: AttnBatch, device="cuda:0"):
+def attn_workspace(desc: VQAttnDesc, batch: AttnBatch, device=None):
     """A workspace for vq_attn_decode and vq_attn_prompt, ready for use: for this batch and every one of no more sequences, new tokens
-    and max_len."""
+    and max_len.  device: the batch's, if it is not given."""
     import torch
-    return torch.zeros(vq_attn_workspace_bytes(desc, batch), dtype=torch.uint8, device=device)
+    return torch.zeros(vq_attn_workspace_bytes(desc, batch), dtype=torch.uint8, device=batch.device if device is None else device)
 
 
 def _attn(call, name, desc, batch, q, k_pages, v_pages, out, workspace, lse, stream):

@@ -1,0 +1,22 @@
+"""The page pool where something goes wrong, or lies on another GPU than the current one: nothing it keeps changes, and copies go to its own."""
+import contextlib
+
+import pytest
+import torch
+
+import paper_2402_15319_amd as vq
+from paper_2402_15319_amd import cache as vc
+
+
+def _state(c):
+    return ({s: (c.pages(s), c.length(s)) for s in c._pages}, c.free_pages, sorted(c._free), list(c._holders))
+
+
+def _pool(pages=20, device="cpu"):
+    return vc.PagedCache(2, 2, 1, 64, 16, pages, 6, device=device)
+
+
+def test_a_workspace_lies_where_the_batch_does():
+    desc = vq.make_attn_desc(8, 2, 128, 16, 5)
+    batch = vq.AttnBatch(torch.ones(1, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32), max_len=32)
+    assert vq.attn_workspace(desc, batch).device == torch.device("cpu")
