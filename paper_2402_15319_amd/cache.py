@@ -63,8 +63,9 @@ class PagedCache:
 
     def fork(self, s: int) -> int:
         """A new sequence with the tokens of s, in the same pages."""
+        pages, length = list(self._pages[s]), self._length[s]
         t = self.add()
-        self._pages[t], self._length[t] = list(self._pages[s]), self._length[s]
+        self._pages[t], self._length[t] = pages, length
         for p in self._pages[t]:
             self._holders[p] += 1
         return t

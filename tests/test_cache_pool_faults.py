@@ -16,6 +16,15 @@ def _pool(pages=20, device="cpu"):
     return vc.PagedCache(2, 2, 1, 64, 16, pages, 6, device=device)
 
 
+def test_a_fork_of_nothing_leaves_nothing():
+    c = _pool()
+    a = c.add()
+    with pytest.raises(KeyError):
+        c.fork(a + 7)
+    assert list(c._pages) == list(c._length) == [a]
+    assert c.fork(a) == a + 1
+
+
 def test_a_workspace_lies_where_the_batch_does():
     desc = vq.make_attn_desc(8, 2, 128, 16, 5)
     batch = vq.AttnBatch(torch.ones(1, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32), max_len=32)
