@@ -100,18 +100,26 @@ class PagedCache:
             want += copy + need - have
         if want > len(self._free):
             raise OutOfPages(f"{want} pages wanted, {len(self._free)} free")
-        pairs = []
-        for s, n, copy, more in plan:
-            own = self._pages[s]
-            if copy:
-                page = self._take()
-                self._holders[own[-1]] -= 1
-                pairs.append((own[-1], page))
-                own[-1] = page
-            own.extend(self._take() for _ in range(more))
-            self._length[s] += n
+        taken = [heapq.heappop(self._free) for _ in range(want)]
+        ahead = iter(taken)
+        chosen = [(next(ahead) if copy else None, [next(ahead) for _ in range(more)]) for _, _, copy, more in plan]
+        pairs = [(self._pages[s][-1], page) for (s, _, _, _), (page, _) in zip(plan, chosen) if page is not None]
         if pairs:
-            vq_cache_copy(self.desc, self._buffers, pairs, stream=stream)
+            try:
+                vq_cache_copy(self.desc, self._buffers, pairs, stream=stream)
+            except BaseException:
+                for page in taken:
+                    heapq.heappush(self._free, page)
+                raise
+        for (s, n, _, _), (page, more) in zip(plan, chosen):
+            own = self._pages[s]
+            if page is not None:
+                self._holders[own[-1]] -= 1
+                own[-1] = page
+            own.extend(more)
+            self._length[s] += n
+        for page in taken:
+            self._holders[page] = 1
 
     def compact(self, stream=None) -> int:
         """Moves the pages in use to the lowest numbers; how many moved.  Batches made before list the old numbers."""
@@ -128,11 +136,6 @@ class PagedCache:
                 self._holders[b], self._holders[a] = self._holders[a], 0
         self._free = list(range(used, self.n_pages))   # sorted, so a heap
         return len(pairs)
-
-    def _take(self) -> int:
-        p = heapq.heappop(self._free)
-        self._holders[p] = 1
-        return p
 
     # ------------------------------------------------------------------ calls
     def batch(self, sequences, new=None) -> AttnBatch:

@@ -25,6 +25,30 @@ def test_a_fork_of_nothing_leaves_nothing():
     assert c.fork(a) == a + 1
 
 
+def test_a_copy_that_fails_changes_nothing(monkeypatch):
+    def broken(*a, **k):
+        raise vq.VQError(-5, "vq_cache_copy")
+    c = _pool()
+    a, other = c.add(), c.add()
+    c.grow([other, a], [40, 20])
+    c.fork(a)
+    d = c.add()
+    c.grow([d], [5])
+    c.free(other)          # holes for a compaction
+    before = _state(c)
+    monkeypatch.setattr(vc, "vq_cache_copy", broken)
+    with pytest.raises(vq.VQError):
+        c.grow([d, a], [40, 30])
+    assert _state(c) == before
+    with pytest.raises(vq.VQError):
+        c.compact()
+    assert _state(c) == before
+    monkeypatch.setattr(vc, "vq_cache_copy", lambda *a, **k: None)
+    assert c.compact() > 0
+    c.grow([d, a], [40, 30])
+    assert c.length(a) == 50 and _state(c) != before
+
+
 def test_a_workspace_lies_where_the_batch_does():
     desc = vq.make_attn_desc(8, 2, 128, 16, 5)
     batch = vq.AttnBatch(torch.ones(1, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32), max_len=32)
