@@ -4,10 +4,11 @@ Sequences take pages from one pool as they grow, share them after a fork, give t
 several sequences share is copied when one of them writes into it; compaction moves the pages in use to the lowest numbers.
 Buffers, copies and the batches for the attention calls go by the same page numbers in every layer.
 
-Copies are enqueued on the stream given (the current one by default): use the cache on one stream, or order the streams.
+Copies are enqueued on the stream given (by default the current one of the cache's GPU): use the cache on one stream, or order the streams.
 """
 from __future__ import annotations
 
+import contextlib
 import heapq
 
 import torch
@@ -106,7 +107,7 @@ class PagedCache:
         pairs = [(self._pages[s][-1], page) for (s, _, _, _), (page, _) in zip(plan, chosen) if page is not None]
         if pairs:
             try:
-                vq_cache_copy(self.desc, self._buffers, pairs, stream=stream)
+                self._copy(pairs, stream)
             except BaseException:
                 for page in taken:
                     heapq.heappush(self._free, page)
@@ -128,7 +129,7 @@ class PagedCache:
         moved = [p for p in range(used, self.n_pages) if self._holders[p]]
         pairs = list(zip(moved, holes))
         if pairs:
-            vq_cache_copy(self.desc, self._buffers, pairs, stream=stream)
+            self._copy(pairs, stream)
             to = dict(pairs)
             for own in self._pages.values():
                 own[:] = [to.get(p, p) for p in own]
@@ -136,6 +137,11 @@ class PagedCache:
                 self._holders[b], self._holders[a] = self._holders[a], 0
         self._free = list(range(used, self.n_pages))   # sorted, so a heap
         return len(pairs)
+
+    def _copy(self, pairs, stream) -> None:
+        device = torch.device(self.device)
+        with torch.cuda.device(device) if device.type == "cuda" else contextlib.nullcontext():
+            vq_cache_copy(self.desc, self._buffers, pairs, stream=stream)
 
     # ------------------------------------------------------------------ calls
     def batch(self, sequences, new=None) -> AttnBatch:

@@ -49,6 +49,28 @@ def test_a_copy_that_fails_changes_nothing(monkeypatch):
     assert c.length(a) == 50 and _state(c) != before
 
 
+def test_copies_are_enqueued_on_the_pool_s_gpu(monkeypatch):
+    current, at = [0], []
+
+    @contextlib.contextmanager
+    def device(d):
+        before, current[0] = current[0], torch.device(d).index
+        yield
+        current[0] = before
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(vc, "vq_cache_copy", lambda *a, **k: at.append(current[0]))
+    c = _pool()
+    c.device = torch.device("cuda:1")     # the buffers stay on the host: nothing is copied here
+    a = c.add()
+    c.grow([a], [20])
+    b = c.fork(a)
+    c.grow([b], [1])
+    assert at == [1] and current == [0]
+    c.free(a)
+    c.compact()
+    assert set(at) == {1} and current == [0]
+
+
 def test_a_workspace_lies_where_the_batch_does():
     desc = vq.make_attn_desc(8, 2, 128, 16, 5)
     batch = vq.AttnBatch(torch.ones(1, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32), max_len=32)
