@@ -16,7 +16,7 @@ namespace {
 // TILES: more than 16 query heads share what is read of their key/value head (64 sequences of 4,096 to 8,192, 48 heads to one of 128: 63 us,
 // 115 a tile to a workgroup).
 template <bool BF16, int D, bool WHOLE_LINES, int kWaves, int TILES>
-__global__ __launch_bounds__(64 * kWaves, D == 256 && kWaves == 4 ? 1 : 2) void decode_kernel(const DecodeArgs A) {
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void decode_kernel(const DecodeArgs A) {
   constexpr int KS = D / 32, DT = D / 16;
   const AttnArgs& a = A.a;
   const int part = blockIdx.z, s = blockIdx.y;
@@ -412,9 +412,9 @@ void launch_pages(const DecodeArgs& a, dim3 grid, hipStream_t s) {
   if constexpr (D <= kTogetherDim) {
     if (a.plan.together == 3) return decode_kernel<BF16, D, WHOLE_LINES, 4, 3><<<grid, 256, 0, s>>>(a);
     if (a.plan.together == 2) return decode_kernel<BF16, D, WHOLE_LINES, 4, 2><<<grid, 256, 0, s>>>(a);
+    if (a.plan.waves == 8) return decode_kernel<BF16, D, WHOLE_LINES, 8, 1><<<grid, 512, 0, s>>>(a);   // the plan has none for larger heads
   }
-  if (a.plan.waves == 8) decode_kernel<BF16, D, WHOLE_LINES, 8, 1><<<grid, 512, 0, s>>>(a);
-  else decode_kernel<BF16, D, WHOLE_LINES, 4, 1><<<grid, 256, 0, s>>>(a);
+  decode_kernel<BF16, D, WHOLE_LINES, 4, 1><<<grid, 256, 0, s>>>(a);
 }
 
 template <bool BF16, int D>
