@@ -298,7 +298,8 @@ typedef struct vq_attn_desc {
   int32_t page_size;    /* tokens in a page: 16, 32, 64 or 128                        */
   int32_t n_pages;      /* pages in a K or V buffer                                   */
   int32_t dtype;        /* VQ_F16 or VQ_BF16: q, k, v, the cache and out              */
-  float scale;          /* of the logits: positive and finite, as 1 / sqrt(head_dim)  */
+  float scale;          /* of the logits: positive, at most 2.35e38 (scale * log2(e) is
+                           finite), as 1 / sqrt(head_dim)                             */
   int32_t reserved;     /* 0                                                          */
 } vq_attn_desc;
 

@@ -13,6 +13,8 @@ bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
 int hip_status(hipError_t e) { return e == hipSuccess ? VQ_OK : VQ_ERR_HIP; }
 
+constexpr float kLog2E = 1.44269504088896f;
+
 int check_attn_desc(const vq_attn_desc* d, bool scaled) {
   if (!d) return VQ_ERR_NULL;
   if (d->heads < 1 || d->kv_heads < 1 || d->head_dim < 1 || d->page_size < 1 || d->n_pages < 1 || d->reserved != 0) return VQ_ERR_BAD_DESC;
@@ -21,7 +23,7 @@ int check_attn_desc(const vq_attn_desc* d, bool scaled) {
   if (d->head_dim != 64 && d->head_dim != 96 && d->head_dim != 128 && d->head_dim != 256) return VQ_ERR_UNSUPPORTED;
   if (d->page_size != 16 && d->page_size != 32 && d->page_size != 64 && d->page_size != 128) return VQ_ERR_UNSUPPORTED;
   if (d->dtype != VQ_F16 && d->dtype != VQ_BF16) return VQ_ERR_UNSUPPORTED;
-  if (scaled && !(d->scale > 0.f && d->scale <= 3.402823466e38f)) return VQ_ERR_BAD_ARG;   // a NaN fails both
+  if (scaled && !(d->scale > 0.f && d->scale * kLog2E <= 3.402823466e38f)) return VQ_ERR_BAD_ARG;   // a NaN fails both
   return VQ_OK;
 }
 
@@ -243,7 +245,7 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   a.lse = lse_f32;
   a.heads = desc->heads;
   a.group = desc->heads / desc->kv_heads;
-  a.scale_log2 = desc->scale * 1.44269504088896f;
+  a.scale_log2 = desc->scale * kLog2E;
   const bool bf16 = desc->dtype == VQ_BF16;
   if (!decode) {
     const PromptArgs prompt = {a, prompt_plan(*desc, *batch), (uint32_t*)workspace, (float*)workspace + kJoinCounters};
