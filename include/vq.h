@@ -320,9 +320,10 @@ typedef struct vq_attn_batch {
   const int32_t* page_table;  /* [n_seqs][table_width]; entries beyond a sequence's length are not read */
 } vq_attn_batch;
 
-/* Element strides of a [token][head][dim] array.  Two orders are read and written in whole vectors: dim = 1 with token
- * and head multiples of 8, and token = 1 with dim and head multiples of 8 (a product Y[features, tokens] of
- * vq_gemm_batched with row stride ldy is token = 1, head = head_dim * ldy, dim = ldy); others an element at a time.
+/* Element strides of a [token][head][dim] array.  Rows with dim = 1 and token and head multiples of 8 are 16-byte aligned, and
+ * read and written in whole vectors; others begin at any element, and attention reads and writes an element at a time (a
+ * product Y[features, tokens] of vq_gemm_batched with row stride ldy is token = 1, head = head_dim * ldy, dim = ldy;
+ * vq_cache_append reads it along the tokens in whole vectors).
  * Where there is one token, or one head, its stride is not looked at.  A NULL vq_strides means
  * [token][heads][head_dim] without gaps.  Inputs may repeat rows (stride 0); elements of an output are distinct. */
 typedef struct vq_strides { int64_t token, head, dim; } vq_strides;
@@ -333,8 +334,8 @@ VQ_API int vq_cache_bytes(const vq_attn_desc* desc, size_t* bytes);
 /*
  * The new tokens' keys and values into their pages, copied bit for bit; k and v are
  * [n_tokens][kv_heads][head_dim] with the strides given.  Tokens with a negative position, with one
- * of max_len or more, or in a page outside the cache, are left out.  k, v, k_pages and v_pages are 16-byte aligned and do not
- * overlap.  desc->scale is not used.  One launch.
+ * of max_len or more, or in a page outside the cache, are left out.  k_pages and v_pages are 16-byte aligned; the arrays do
+ * not overlap.  desc->scale is not used.  One launch.
  */
 VQ_API int vq_cache_append(const vq_attn_desc* desc, const vq_attn_batch* batch,
                            const void* k, const vq_strides* k_strides,
@@ -364,7 +365,7 @@ VQ_API int vq_attn_workspace_bytes(const vq_attn_desc* desc, const vq_attn_batch
 /*
  * out[token][head][dim] for one new token of every sequence (n_tokens = n_seqs; q_start is not
  * read), whose key and value are in the cache already.  lse_f32 (may be NULL): fp32
- * [n_tokens][heads].  q and out are 16-byte aligned and must not alias.  The same call gives the
+ * [n_tokens][heads].  q and out must not alias.  The same call gives the
  * same bits every time.
  */
 VQ_API int vq_attn_decode(const vq_attn_desc* desc, const vq_attn_batch* batch,

@@ -89,6 +89,11 @@ int check_strides(const vq_strides* in, int n_tokens, int heads, int head_dim, b
   return VQ_OK;
 }
 
+// Rows that the kernels take in whole vectors begin at 16 bytes; of others they take an element at a time, from any.
+bool aligned_rows(const void* p, const Strides& s) {
+  return s.dim == 1 && ((s.token | s.head) & 7) == 0 ? aligned16(p) : ((uintptr_t)p & 1) == 0;
+}
+
 constexpr int kPartStep = 128;            // tokens that a workgroup takes at a time
 constexpr int64_t kEnoughUnits = 256;     // workgroups: one for each CU
 constexpr int64_t kTogetherUnits = 16;
@@ -228,7 +233,7 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   st = check_batch(*desc, batch, decode);
   if (st != VQ_OK) return st;
   if (!q || !k_pages || !v_pages || !out || !workspace) return VQ_ERR_NULL;
-  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(workspace) || !aligned4(lse_f32)) return VQ_ERR_ALIGN;
+  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(workspace) || !aligned4(lse_f32)) return VQ_ERR_ALIGN;
   if (q == out || k_pages == out || v_pages == out) return VQ_ERR_BAD_ARG;
   DecodeArgs both = {};
   AttnArgs& a = both.a;
@@ -236,6 +241,7 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   if (st != VQ_OK) return st;
   st = check_strides(out_strides, batch->n_tokens, desc->heads, desc->head_dim, true, &a.os);
   if (st != VQ_OK) return st;
+  if (!aligned_rows(q, a.qs) || !aligned_rows(out, a.os)) return VQ_ERR_ALIGN;
   if (workspace_bytes < vq::workspace(*desc, *batch)) return VQ_ERR_BAD_ARG;
   a.c = cache_args(*desc, *batch, decode);
   a.q = (const uint16_t*)q;
@@ -279,13 +285,14 @@ int vq_cache_append(const vq_attn_desc* desc, const vq_attn_batch* batch, const 
   st = check_batch(*desc, batch, false);
   if (st != VQ_OK) return st;
   if (!k || !v || !k_pages || !v_pages) return VQ_ERR_NULL;
-  if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages)) return VQ_ERR_ALIGN;
+  if (!aligned16(k_pages) || !aligned16(v_pages)) return VQ_ERR_ALIGN;
   if (k_pages == v_pages || k == k_pages || k == v_pages || v == k_pages || v == v_pages) return VQ_ERR_BAD_ARG;
   AppendArgs a = {};
   st = check_strides(k_strides, batch->n_tokens, desc->kv_heads, desc->head_dim, false, &a.ks);
   if (st != VQ_OK) return st;
   st = check_strides(v_strides, batch->n_tokens, desc->kv_heads, desc->head_dim, false, &a.vs);
   if (st != VQ_OK) return st;
+  if (!aligned_rows(k, a.ks) || !aligned_rows(v, a.vs)) return VQ_ERR_ALIGN;
   a.c = cache_args(*desc, *batch, false);
   a.k = (const uint16_t*)k;
   a.v = (const uint16_t*)v;
