@@ -390,6 +390,8 @@ def vq_cache_copy(desc: VQAttnDesc, buffers, from_to, stream=None) -> None:
         flat = array.array("i", [p for a, b in from_to for p in (a, b)])
     except (ValueError, TypeError, OverflowError) as e:
         raise ValueError("vq_cache_copy: from_to is a list of pairs of page numbers") from e
+    if not isinstance(buffers, (list, tuple)):
+        buffers = list(buffers)   # gone through twice where there are addresses among them
     try:
         at = array.array("Q", [b.data_ptr() for b in buffers])
     except AttributeError:
