@@ -195,7 +195,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void decode_kernel(c
 #pragma unroll
       for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[n][i][j] = __builtin_isunordered(o[n][i][j], o[n][i][j]) ? 0.f : o[n][i][j];
+        for (int j = 0; j < 4; ++j) o[n][i][j] = __builtin_isunordered(o[n][i][j], o[n][i][j]) ? kUnknown : o[n][i][j];
     if constexpr (TILES * D >= 3 * 128) {   // q once more, or the loop above spills more of it for its sake (64 sequences, 48 heads to one: 75 us for 70)
       asm volatile("" ::: "memory");
       load_q();
@@ -231,6 +231,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void decode_kernel(c
         for (int n = 0; n < TILES; ++n) o[n][i] = mfma16<BF16>(vf[i], there[n], o[n][i]);
       }
     }
+#pragma unroll
+    for (int n = 0; n < TILES; ++n)
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[n][i][j] = o[n][i][j] == kUnknown ? __builtin_nanf("") : o[n][i][j];
   }
 
   // The waves' sums, brought to one maximum: four values of a head a thread.

@@ -123,6 +123,10 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // outputs of bf16 close to their smallest do not feel it.)
 __device__ __forceinline__ float rescale(float from, float to) { return fmaxf(exp2_fast(from - to), 0x1p-149f); }
 
+// Stands for a sum that is no number while the values that are none are looked for; where there are none, the sum went beyond
+// the range of its 32 bits, and is no number in the end.
+constexpr float kUnknown = 0x1.5a5a5ap-120f;
+
 // The halves of a dword that are no finite numbers: all ones.
 template <bool BF16> __device__ __forceinline__ uint32_t odd_halves(uint32_t v) {
   constexpr uint32_t kExp = BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = BF16 ? 0x00800080u : 0x04000400u;

@@ -80,3 +80,23 @@ def test_infinite_values_with_next_to_no_weight(shape, dim, dtype, falls, rise):
     with np.errstate(invalid="ignore"):
         over = (np.abs(got - want) > b_out) & np.isfinite(want)
     assert not over.any()
+
+
+@pytest.mark.parametrize("call, lens, new", [("decode", [700] * 128, None), ("decode", [700], None), ("prompt", [300], [300]), ("prompt", [3000], [5])])
+def test_sums_beyond_the_range_stay_visible(call, lens, new):
+    """Values close to bf16's largest: their sum is infinite, and no number once a later token leaves it next to no weight.  Neither
+    may come out as a finite value made up for it."""
+    p = Problem(4, 2, 64, 16, "bf16", lens, new, seed=1)
+    p.q_host[:, :, 0] = 1.0 / p.scale
+    rise = lens[0] - 100
+    for t in range(lens[0]):
+        pages, slot = p.table[:, t // 16], t % 16
+        p.k_host[pages, :, slot, 0] = 250.0 if t == rise else 0.0
+        p.v_host[pages, 1, 3, slot] = 3.3e38 if t < 100 else 1.0
+    p.k_pages, p.v_pages, p.q = p.k_host.to(p.dev), p.v_host.to(p.dev), p.rows(p.q_host, p.heads)
+    out, _ = run(p, call)
+    got = out.double().cpu().numpy()
+    above = got[-1, 2:, 3]
+    assert (~np.isfinite(above) | (np.abs(above - 1.0) < 0.02)).all(), above
+    finite = np.delete(got, 3, axis=2)
+    assert np.isfinite(finite).all()
