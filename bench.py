@@ -31,8 +31,8 @@ HBM_PEAK_GBS = 8000.0          # MI355X published HBM3E bandwidth
 # rocprofv3 --pmc FETCH_SIZE / WRITE_SIZE scaled by a copy kernel of known size; the summary
 # and the commands are in profiles/gemv_stream_k16_llama7b_pass.md.  The figure belongs to one
 # build of the kernel: it is reported only while the library still has the version it was
-# measured on (vq_version() is raised whenever a kernel, the device layout or the set of entry
-# points changes).
+# measured on (vq_version() is raised whenever a kernel of the weight products, the device layout
+# or a signature changes).
 TRAFFIC_BYTES_PER_LAUNCH = 1857703283
 TRAFFIC_MEASURED_ON_VERSION = 3
 MFMA_F16_PEAK_TFLOPS = 2500.0  # MI355X published dense fp16 matrix peak

@@ -289,7 +289,8 @@ VQ_API int vq_em_update(const vq_desc* desc, const void* W_f32, const void* hdia
  *     out = sum exp(t_j - m) v_j / l           lse = m + ln l
  * A row without any token to attend (p < 0) has out = 0 and lse = -infinity.  Query head h reads
  * key/value head h / (heads / kv_heads).  Products are accumulated, and m, l and the sums held, in
- * fp32; exp(t_j - m) is rounded to the cache's type for the second product, out once at the end.
+ * fp32; exp(t_j - m) is rounded to the cache's type for the second product, out once at the end.  Values that
+ * are no numbers go through the formula all the same: a weight that rounds to 0 still makes infinity of an infinite v.
  */
 typedef struct vq_attn_desc {
   int32_t heads;        /* query heads, at most 1024                                  */

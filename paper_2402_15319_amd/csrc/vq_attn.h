@@ -51,7 +51,7 @@ struct DecodePlan {
   int32_t waves;          // of a workgroup: 4 or 8; each takes 32 tokens in turn
 };
 constexpr int kJoinCounters = 16384;   // at the start of the workspace: parts that have finished, zero between calls
-constexpr int kTileHeads = 16, kTogetherDim = 128;   // several tiles up to this head_dim: the sums of larger ones leave no registers for it
+constexpr int kTileHeads = 16, kTogetherDim = 128;   // several tiles up to this head_dim: two of larger ones do not fit the registers (three of 128 spill 80 bytes)
 constexpr int kMostParts = 64;         // of a sequence
 
 struct DecodeArgs {

@@ -95,7 +95,9 @@ bool aligned_rows(const void* p, const Strides& s) {
 }
 
 constexpr int kPartStep = 128;            // tokens that a workgroup takes at a time
-constexpr int64_t kEnoughUnits = 256;     // workgroups: one for each CU
+// Workgroups: one for each CU.  The plans count on 256 CUs rather than on the device's: they follow from sizes alone, so that a
+// workspace can be asked for without a device.
+constexpr int64_t kEnoughUnits = 256;
 constexpr int64_t kTogetherUnits = 16;
 constexpr int kLongPart = 4096, kShortPart = 1024;
 constexpr int kShortValues = 32768;       // of a sequence's keys: no parts up to here
@@ -107,7 +109,8 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   p.cols = group < kTileHeads ? group : kTileHeads;
   p.together = d.head_dim > kTogetherDim || p.tiles == 1 ? 1 : p.tiles == 2 || p.tiles == 4 ? 2 : 3;
   // Three tiles together read a key/value head once, but leave one workgroup to join all of their parts: with 48 heads to one of 128 and
-  // sequences of up to 8,192, 64 of them take 63 us (a tile to a workgroup 115), 32 42 (74), 16 46 (43) and 8 50 (29).
+  // sequences of 4,096 to 8,192, 64 of them take 59 us (a tile to a workgroup 118) and 32 36 (76); with fewer the join is longer than what
+  // it saves (16 46 us and 43, 8 50 and 28).
   if ((int64_t)b.n_seqs * d.kv_heads * ((p.tiles + p.together - 1) / p.together) < kTogetherUnits) p.together = 1;
   const int64_t units = (int64_t)b.n_seqs * d.kv_heads * ((p.tiles + p.together - 1) / p.together);
   const int64_t steps = b.max_len > kPartStep ? ((int64_t)b.max_len + kPartStep - 1) / kPartStep : 1;
@@ -118,10 +121,11 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
     // us, in two parts of 4 waves 7.7; of 512 8.9 and 8.0; of 512 x 32 heads of 64 5.6 and 7.7).
     p.waves = b.max_len > 32 * p.waves && p.together == 1 ? 8 : 4;
   } else if (units * p.together <= kJoinCounters) {
-    // A workgroup for every CU is enough where they are of one size (130,001 tokens x 8 heads: 256 workgroups 97 us, 512 100,
-    // 1,024 106).  Where there are as many without a split, the lengths will differ, and parts of 1,024 tokens even them
-    // out (61 sequences of 1 to 8,192: parts of 512 61 us, of 1,024 66, before q came through LDS 68, of 2,048 77 then; 61 of 4,000 each:
-    // parts of 512 194 us, of 1,024 177).
+    // Fewer workgroups than CUs: as many parts as fill the chip once, up to 4,096 tokens each (130,001 tokens x 8 heads: 256
+    // workgroups 97 us, 512 100, 1,024 106).  As many without a split: parts of 1,024 tokens, which even out what the lengths differ
+    // by (61 sequences of 1 to 8,192: parts of 512 61 us, of 1,024 66; 61 of 4,000 each: parts of 512 194 us, of 1,024
+    // 177).  Lengths can differ in the first case too, and only max_len is known here: 31 sequences of 1 to 8,192 x 8 heads have two
+    // parts each and take 50 us, 32 of them eight and 58.
     const int64_t most = units < kEnoughUnits ? kLongPart : kShortPart;
     const int64_t enough = (kEnoughUnits + units - 1) / units, least = (steps * kPartStep + most - 1) / most;
     parts = (least + enough - 1) / enough * enough;   // as many for every CU
@@ -160,8 +164,11 @@ PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   // Two workgroups of one team share a compute unit and run a step each in about 2.1 us; one alone takes 1.3 us a step.  Where there is but
   // one for each compute unit, or where two are gone through long before the last, two teams take a tile's steps in turn.  Theirs is one
   // barrier, which keeps both at the same work and costs a long prompt 14 %.  Three workgroups on heads of 64 share a compute unit: those keep
-  // one team where parts are long.  (32 heads of 128, prompts of 768, 1,024 and 1,500: 24.6, 29.3 and 40.0 us with one team, 20.4, 24.9 and
-  // 36.1 with two; two chunks behind 12,000 tokens, heads of 64: 72 us with one, 96 with two.)
+  // one team where parts are long.  (`lone`: 32 heads of 128, prompts of 768 and 1,024: 24.6 and 29.3 us with one team, 20.4 and 24.9 with two;
+  // two chunks behind 12,000 tokens, heads of 64: 72 us with one, 96 with two.  `few`: 32 heads of 128, 1,500, 1,800 and 2,048 tokens: 41.5, 49.4
+  // and 57.4 with one, 37.3, 48.8 and 55.4 with two; of 64 25.2 and 21.9 at 1,500.  Its lines of 24 and 32 steps enclose what was
+  // measured first, and are not where one team becomes the faster: 32 heads and 1,100 tokens take 30.4 us with one and would take 27.3, 16
+  // heads and 3,000 67.7 and 57.5, but 8 heads and 4,500 67.8 and 74.1.)
   const int64_t full = (b.n_tokens + (int64_t)p.tokens - 1) / p.tokens * (d.heads / p.heads);   // tiles, but for those that a sequence does not fill
   const bool lone = full <= 256 && steps >= 8 && (steps <= 32 || d.head_dim > 64), few = full <= 512 && steps >= 24 && steps <= 32;
   p.teams = d.head_dim <= 128 && (lone || few) ? 2 : 1;

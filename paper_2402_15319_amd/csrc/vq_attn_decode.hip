@@ -13,8 +13,8 @@ namespace {
 // caches by (24 sequences of 2,000 to 4,096 tokens x 32 heads, pages of 16: 195 us, 217 without).  In larger pages a step's 64 bytes of a row of
 // V^T are half a line, and the wave with the other half wants it kept (130,001 tokens, pages of 64: 95 us, 107 if not); the
 // same holds for K, whose rows four instructions read in turn.
-// TILES: more than 16 query heads share what is read of their key/value head (64 sequences of 4,096 to 8,192, 48 heads to one of 128: 63 us,
-// 115 a tile to a workgroup).
+// TILES: more than 16 query heads share what is read of their key/value head (64 sequences of 4,096 to 8,192, 48 heads to one of 128: 59 us,
+// 118 a tile to a workgroup).
 template <bool BF16, int D, bool WHOLE_LINES, int kWaves, int TILES>
 __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void decode_kernel(const DecodeArgs A) {
   constexpr int KS = D / 32, DT = D / 16;

@@ -87,7 +87,9 @@ template <bool BF16> __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, 
   else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// Eight weights rounded to the cache's type.
+// Eight weights rounded to the cache's type: a matrix instruction takes both operands in one 16-bit type, and a weight in two halves
+// would double the second product (long prompts are bound by their products).  Each weight is off by 2^-11 (fp16) or 2^-8 (bf16)
+// of itself at most, the sum of the weights not: out has about that error again beside its own last rounding.
 template <bool BF16> __device__ __forceinline__ u32x4 pack8(f32x8 p) {
   if constexpr (BF16) return __builtin_bit_cast(u32x4, __builtin_convertvector(p, bf16x8));
   else return __builtin_bit_cast(u32x4, __builtin_convertvector(p, f16x8));
