@@ -1,10 +1,11 @@
 """The attention block of a decoder layer on vector-quantised weights: prompts, then tokens one at a time, with a fork.
 
-    python examples/attention_block.py [--tokens 512] [--steps 16] [--continuations 3]
+    python examples/attention_block.py [--tokens 512] [--steps 16] [--continuations 3] [--bits 8] [--window 256 --sinks 4]
 
 The q, k, v and o matrices are packed indices and codebooks; their products run straight into the paged cache and out of it:
 vq_gemm_batched writes [features, tokens], whose strides vq_cache_append, vq_attn_prompt and vq_attn_decode take as they are, and
-the next product reads what attention wrote.  One user's prompt is forked into several continuations, which share its pages.
+the next product reads what attention wrote.  One user's prompt is forked into several continuations, which share its pages.  The
+cache can be held in 8 bits, and tokens can see a window and a few first ones; pages behind the window then go back to the pool.
 """
 from __future__ import annotations
 
@@ -50,12 +51,15 @@ class AttentionBlock:
         """The same values as [token][head][dim]."""
         return y.unflatten(0, (heads, self.head_dim)).permute(2, 0, 1)
 
-    def __call__(self, x, cache: PagedCache, layer: int, batch, workspace, prompt: bool):
+    def __call__(self, x, cache: PagedCache, layer: int, batch, workspace, prompt: bool, window=None):
         q, k, v = self.product("q", x), self.product("k", x), self.product("v", x)
         vq.vq_cache_append(cache.desc, batch, self.by_heads(k, self.kv_heads), self.by_heads(v, self.kv_heads), cache.k[layer], cache.v[layer])
         out = torch.empty(self.width, x.stride(0), dtype=torch.float16, device=DEV)[:, :x.shape[1]]
-        call = vq.vq_attn_prompt if prompt else vq.vq_attn_decode
-        call(cache.desc, batch, self.by_heads(q, self.heads), cache.k[layer], cache.v[layer], self.by_heads(out, self.heads), workspace)
+        args = self.by_heads(q, self.heads), cache.k[layer], cache.v[layer], self.by_heads(out, self.heads), workspace
+        if window is None:
+            (vq.vq_attn_prompt if prompt else vq.vq_attn_decode)(cache.desc, batch, *args)
+        else:
+            (vq.vq_attn_prompt_window if prompt else vq.vq_attn_decode_window)(cache.desc, batch, window, *args)
         return x + self.product("o", out)
 
 
@@ -66,12 +70,15 @@ def columns(x):
     return t[:, :x.shape[1]]
 
 
-def generate(block: AttentionBlock, prompts, steps: int, continuations: int, page_size: int = 16):
+def generate(block: AttentionBlock, prompts, steps: int, continuations: int, page_size: int = 16, bits: int = 16, window=None):
     """prompts: [width, tokens] inputs of each user.  The first user's prompt is continued `continuations` times.  Returns every
-    sequence's outputs, [width, its tokens], in the order of the users with the further continuations behind them."""
+    sequence's outputs, [width, its tokens], in the order of the users with the further continuations behind them.  bits: 8 or 16, of
+    the cache; window: a VQAttnWindow, or None."""
+    more = {} if window is None else dict(window=window)
     longest = max(p.shape[1] for p in prompts) + steps
     per = -(-longest // page_size)
-    cache = PagedCache(1, block.heads, block.kv_heads, block.head_dim, page_size, per * (len(prompts) + continuations), per)
+    cache = PagedCache(1, block.heads, block.kv_heads, block.head_dim, page_size, per * (len(prompts) + continuations), per,
+                       cache_dtype=vq.VQ_E4M3 if bits == 8 else None)
     seqs, new = [cache.add() for _ in prompts], [p.shape[1] for p in prompts]
     users = len(prompts) + max(0, continuations - 1)
     ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=DEV)  # noqa: E731
@@ -79,7 +86,7 @@ def generate(block: AttentionBlock, prompts, steps: int, continuations: int, pag
     workspace = vq.attn_workspace(cache.desc, largest, DEV)   # serves every smaller batch
     cache.grow(seqs, new)
     batch = cache.batch(seqs, new)
-    y = block(columns(torch.cat(list(prompts), dim=1)), cache, 0, batch, workspace, prompt=True)
+    y = block(columns(torch.cat(list(prompts), dim=1)), cache, 0, batch, workspace, prompt=True, **more)
     outputs = [[part] for part in y.split(new, dim=1)]
     for _ in range(continuations - 1):
         seqs.append(cache.fork(seqs[0]))
@@ -91,7 +98,9 @@ def generate(block: AttentionBlock, prompts, steps: int, continuations: int, pag
         # a real decoder goes on from a sampled token's embedding; here each sequence goes its way by some noise
         x = torch.stack([o[-1][:, -1] for o in outputs], dim=1)
         x = 0.5 * x + 0.5 * torch.randn(x.shape, device=DEV, dtype=x.dtype, generator=gen)
-        y = block(columns(x), cache, 0, batch, workspace, prompt=False)
+        y = block(columns(x), cache, 0, batch, workspace, prompt=False, **more)
+        if window is not None:
+            cache.slide(seqs, window.window, window.sinks)
         for i, o in enumerate(outputs):
             o.append(y[:, i:i + 1])
     if len(seqs) > 2:       # a user leaves; what remains moves together
@@ -105,11 +114,15 @@ def main():
     ap.add_argument("--tokens", type=int, default=512)
     ap.add_argument("--steps", type=int, default=16)
     ap.add_argument("--continuations", type=int, default=3)
+    ap.add_argument("--bits", type=int, choices=(8, 16), default=16, help="of the cache")
+    ap.add_argument("--window", type=int, help="tokens that a token sees, itself included (default: all)")
+    ap.add_argument("--sinks", type=int, default=0, help="first tokens that stay visible behind the window")
     a = ap.parse_args()
     block = AttentionBlock(32, 32, 128)
     gen = torch.Generator(device=DEV).manual_seed(0)
     prompts = [torch.randn(block.width, n, device=DEV, generator=gen).half() for n in (a.tokens, max(1, a.tokens // 3))]
-    outputs, cache = generate(block, prompts, a.steps, a.continuations)
+    window = None if a.window is None else vq.VQAttnWindow(a.window, a.sinks)
+    outputs, cache = generate(block, prompts, a.steps, a.continuations, bits=a.bits, window=window)
     torch.cuda.synchronize()
     for i, y in enumerate(outputs):
         print(f"sequence {i}: {y.shape[1]} tokens, rms {y.float().square().mean().sqrt():.3f}")

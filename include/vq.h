@@ -94,7 +94,7 @@ typedef enum vq_status {
 
 /* VQ_I8 as codebook_dtype: int8 lookup tables with one fp16 scale per group (Sec. 3.1);
  * VQ_I8_BN: the same plus blockwise normalisation (see the canonical format above). */
-typedef enum vq_dtype { VQ_F16 = 1, VQ_F32 = 2, VQ_I8 = 3, VQ_I8_BN = 4, VQ_BF16 = 5 /* attention only */ } vq_dtype;
+typedef enum vq_dtype { VQ_F16 = 1, VQ_F32 = 2, VQ_I8 = 3, VQ_I8_BN = 4, VQ_BF16 = 5, VQ_E4M3 = 6 /* attention only */ } vq_dtype;
 
 /* Shape of one vector-quantised matrix (Sec. 2.1, Sec. 3.1, Sec. 4). */
 typedef struct vq_desc {
@@ -301,8 +301,26 @@ typedef struct vq_attn_desc {
   int32_t dtype;        /* VQ_F16 or VQ_BF16: q, k, v, the cache and out              */
   float scale;          /* of the logits: positive, at most 2.35e38 (scale * log2(e) is
                            finite), as 1 / sqrt(head_dim)                             */
-  int32_t reserved;     /* 0                                                          */
+  union {
+    int32_t cache_dtype;  /* 0: the pages hold values of dtype; VQ_E4M3: 8-bit codes with scales, below */
+    int32_t reserved;     /* its name where it has to be 0                            */
+  };
 } vq_attn_desc;
+
+/*
+ * Pages in 8 bits (cache_dtype = VQ_E4M3): a value is a code, a number of the 8-bit format with 4 bits of exponent and 3 of
+ * mantissa (largest 448, no infinities), times the scale of its block: 16 successive slots of a page and head, all dimensions.
+ *     K  [n_pages][kv_heads][page_size][head_dim] codes, then fp32 scales [n_pages][kv_heads][page_size / 16]
+ *     V  [n_pages][kv_heads][head_dim][page_size] codes, then scales likewise
+ * A scale is a power of two, and at least 2^-15 (fp16) or 2^-117 (bf16), so that every value of the cache is a number of dtype:
+ * attention is that over a 16-bit cache of these values, no more rounded.
+ *
+ * vq_cache_append rounds.  For each block that gets new tokens, s = the smallest such power of two by which the largest magnitude of their finite
+ * values, taken as 1.875 * 2^15 (fp16; 1.875 * 2^127 for bf16) where it is more, comes to 448 or less; where earlier tokens of
+ * the sequence lie in the block before them, the scale that it has, if that is larger.  Each new value becomes the nearest code
+ * times s (ties to even; magnitudes above 1.875 * 2^15, or 2^127, count as that; NaN and infinities become NaN), and the codes of those earlier
+ * tokens, where the scale grows, are rounded to it in the same way.  Slots behind the new tokens stay as they are.
+ */
 
 /* The sequences of a call.  The three arrays are DEVICE memory and are read by the kernels, so a
  * captured graph follows their contents.  Page numbers outside [0, n_pages) are read as a page
@@ -328,6 +346,10 @@ typedef struct vq_attn_batch {
  * Where there is one token, or one head, its stride is not looked at.  A NULL vq_strides means
  * [token][heads][head_dim] without gaps.  Inputs may repeat rows (stride 0); elements of an output are distinct. */
 typedef struct vq_strides { int64_t token, head, dim; } vq_strides;
+
+/* Which earlier tokens a row attends: the token at position p those at j <= p with j > p - window or j < sinks.  window in [1, 2^29], sinks in
+ * [0, 2^29].  Pages without a token that some row attends are not read for their values, and their table entries may be -1. */
+typedef struct vq_attn_window { int32_t window, sinks; } vq_attn_window;
 
 /* Bytes of the K buffer, and of the V buffer, of one layer's cache (host pointer). */
 VQ_API int vq_cache_bytes(const vq_attn_desc* desc, size_t* bytes);
@@ -382,6 +404,18 @@ VQ_API int vq_attn_prompt(const vq_attn_desc* desc, const vq_attn_batch* batch,
                           const void* k_pages, const void* v_pages,
                           void* out, const vq_strides* out_strides, float* lse_f32,
                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* vq_attn_decode and vq_attn_prompt with a window (not NULL): everything else is theirs, the workspace too. */
+VQ_API int vq_attn_decode_window(const vq_attn_desc* desc, const vq_attn_batch* batch, const vq_attn_window* window,
+                                 const void* q, const vq_strides* q_strides,
+                                 const void* k_pages, const void* v_pages,
+                                 void* out, const vq_strides* out_strides, float* lse_f32,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+VQ_API int vq_attn_prompt_window(const vq_attn_desc* desc, const vq_attn_batch* batch, const vq_attn_window* window,
+                                 const void* q, const vq_strides* q_strides,
+                                 const void* k_pages, const void* v_pages,
+                                 void* out, const vq_strides* out_strides, float* lse_f32,
+                                 void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -18,8 +18,9 @@ __all__ = [
     "vq_status_string", "vq_version", "vq_canonical_bytes", "vq_layout_bytes",
     "vq_pack_layout", "vq_gemv", "vq_gemv_multi", "GemvMultiArgs", "VQLoraDesc", "vq_lora_workspace_bytes", "vq_gemv_lora",
     "vq_gemv_lora_multi", "vq_gemv_lora_multi_static", "vq_gemm_batched", "vq_decode_dense", "vq_em_assign", "vq_em_update",
-    "VQ_BF16", "VQAttnDesc", "VQAttnBatch", "VQStrides", "make_attn_desc", "AttnBatch", "attn_workspace", "vq_cache_bytes",
+    "VQ_BF16", "VQ_E4M3", "VQAttnDesc", "VQAttnBatch", "VQAttnWindow", "VQStrides", "make_attn_desc", "AttnBatch", "attn_workspace", "vq_cache_bytes",
     "vq_cache_append", "vq_cache_copy", "vq_attn_workspace_bytes", "vq_attn_decode", "vq_attn_prompt",
+    "vq_attn_decode_window", "vq_attn_prompt_window",
 ]
 
 VQ_F16 = 1
@@ -27,6 +28,7 @@ VQ_F32 = 2
 VQ_I8 = 3      # codebook_dtype: int8 lookup tables with one fp16 scale per group
 VQ_I8_BN = 4   # the same plus blockwise normalisation (16 levels per group, a 4-bit code per 32 weights)
 VQ_BF16 = 5    # attention over the paged cache only
+VQ_E4M3 = 6    # cache_dtype: 8-bit codes with a scale for each block of 16 slots and head
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libvq.so")
@@ -53,7 +55,16 @@ class VQAttnDesc(ctypes.Structure):
     """Mirror of `vq_attn_desc` (include/vq.h)."""
     _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("dtype", ctypes.c_int32),
-                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+                ("scale", ctypes.c_float), ("cache_dtype", ctypes.c_int32)]
+
+    @property
+    def reserved(self) -> int:
+        """cache_dtype, by its name where it has to be 0."""
+        return self.cache_dtype
+
+    @reserved.setter
+    def reserved(self, value: int) -> None:
+        self.cache_dtype = value
 
 
 class VQAttnBatch(ctypes.Structure):
@@ -61,6 +72,11 @@ class VQAttnBatch(ctypes.Structure):
     _fields_ = [("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("table_width", ctypes.c_int32),
                 ("max_len", ctypes.c_int32), ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
                 ("page_table", ctypes.c_void_p)]
+
+
+class VQAttnWindow(ctypes.Structure):
+    """Mirror of `vq_attn_window` (include/vq.h): a row at position p attends the tokens j <= p with j > p - window or j < sinks."""
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
 class VQStrides(ctypes.Structure):
@@ -136,6 +152,8 @@ def lib() -> ctypes.CDLL:
         for name in ("vq_attn_decode", "vq_attn_prompt"):
             getattr(L, name).restype = i32
             getattr(L, name).argtypes = [ap, bp, vp, st, vp, vp, vp, st, vp, vp, ctypes.c_size_t, vp]
+            getattr(L, name + "_window").restype = i32
+            getattr(L, name + "_window").argtypes = [ap, bp, ctypes.POINTER(VQAttnWindow), vp, st, vp, vp, vp, st, vp, vp, ctypes.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -311,9 +329,9 @@ def vq_em_update(desc: VQDesc, W_f32, hdiag_f32, assign_u8, cb_f32_out, stream=N
 
 
 def make_attn_desc(heads: int, kv_heads: int, head_dim: int, page_size: int, n_pages: int, dtype: int = VQ_F16,
-                   scale: float | None = None) -> VQAttnDesc:
-    """scale: of the logits; None means 1 / sqrt(head_dim)."""
-    return VQAttnDesc(heads, kv_heads, head_dim, page_size, n_pages, dtype, head_dim ** -0.5 if scale is None else scale, 0)
+                   scale: float | None = None, cache_dtype: int | None = None) -> VQAttnDesc:
+    """scale: of the logits; None means 1 / sqrt(head_dim).  cache_dtype: VQ_E4M3 for pages in 8 bits, None for pages of dtype."""
+    return VQAttnDesc(heads, kv_heads, head_dim, page_size, n_pages, dtype, head_dim ** -0.5 if scale is None else scale, cache_dtype or 0)
 
 
 class AttnBatch:
@@ -323,7 +341,7 @@ class AttnBatch:
 
     def __init__(self, kv_len, page_table, n_tokens: int | None = None, max_len: int | None = None, q_start=None, page_size: int | None = None):
         import torch
-        _kinds.update({VQ_F16: torch.float16, VQ_BF16: torch.bfloat16, VQ_F32: torch.float32})
+        _kinds.update({VQ_F16: torch.float16, VQ_BF16: torch.bfloat16, VQ_F32: torch.float32, VQ_E4M3: torch.uint8})
         for what, t, dim in (("kv_len", kv_len, 1), ("page_table", page_table, 2), ("q_start", q_start, 1)):
             if t is not None and (t.dtype != torch.int32 or t.dim() != dim or not t.is_contiguous()):
                 raise ValueError(f"AttnBatch: {what} is a contiguous int32 tensor of {dim} dimension(s)")
@@ -346,7 +364,7 @@ class AttnBatch:
         self._keep = (kv_len, page_table, q_start)
 
 
-_kinds: dict = {}   # VQ_F16, VQ_BF16, VQ_F32: the torch type (filled by the first AttnBatch)
+_kinds: dict = {}   # VQ_F16, VQ_BF16, VQ_F32, VQ_E4M3: the torch type (filled by the first AttnBatch)
 
 
 def _rows(t, n: int, heads: int, dim: int, what: str, kind, gpu: int):
@@ -357,6 +375,12 @@ def _rows(t, n: int, heads: int, dim: int, what: str, kind, gpu: int):
     return None if t.is_contiguous() else VQStrides(*t.stride())
 
 
+def _whole(desc: VQAttnDesc):
+    """Bytes and type of a K or V buffer."""
+    n = desc.n_pages * desc.kv_heads * desc.page_size
+    return (n * desc.head_dim + n // 4, _kinds.get(VQ_E4M3)) if desc.cache_dtype else (2 * n * desc.head_dim, _kinds.get(desc.dtype))
+
+
 def _pages(t, size: int, what: str, kind, gpu: int) -> int:
     """The address of a K or V buffer (an address passes through)."""
     try:
@@ -364,7 +388,7 @@ def _pages(t, size: int, what: str, kind, gpu: int) -> int:
             return t.data_ptr()
     except AttributeError:
         return _ptr(t)
-    raise ValueError(f"{what}: a contiguous tensor of the descriptor's type and of {size} bytes or more on the batch's GPU is wanted, not {t.dtype} "
+    raise ValueError(f"{what}: a contiguous tensor of the descriptor's type (uint8 for pages in 8 bits) and of {size} bytes or more on the batch's GPU is wanted, not {t.dtype} "
                      f"{tuple(t.shape)} on {t.device}")
 
 
@@ -377,10 +401,10 @@ def vq_cache_bytes(desc: VQAttnDesc) -> int:
 def vq_cache_append(desc: VQAttnDesc, batch: AttnBatch, k, v, k_pages, v_pages, stream=None) -> None:
     """k, v: [n_tokens, kv_heads, head_dim] views (strides as vq_strides allows) of the new tokens."""
     n, heads, dim, kind, gpu = batch.n_tokens, desc.kv_heads, desc.head_dim, _kinds.get(desc.dtype), batch.gpu
-    size = 2 * desc.n_pages * heads * desc.page_size * dim
+    size, held = _whole(desc)
     _check(lib().vq_cache_append(desc, batch.struct, k.data_ptr(), _rows(k, n, heads, dim, "k", kind, gpu), v.data_ptr(),
-                                 _rows(v, n, heads, dim, "v", kind, gpu), _pages(k_pages, size, "k_pages", kind, gpu),
-                                 _pages(v_pages, size, "v_pages", kind, gpu), _stream(stream)), "vq_cache_append")
+                                 _rows(v, n, heads, dim, "v", kind, gpu), _pages(k_pages, size, "k_pages", held, gpu),
+                                 _pages(v_pages, size, "v_pages", held, gpu), _stream(stream)), "vq_cache_append")
 
 
 def vq_cache_copy(desc: VQAttnDesc, buffers, from_to, stream=None) -> None:
@@ -412,15 +436,15 @@ def attn_workspace(desc: VQAttnDesc, batch: AttnBatch, device=None):
     return torch.zeros(vq_attn_workspace_bytes(desc, batch), dtype=torch.uint8, device=batch.device if device is None else device)
 
 
-def _attn(call, name, desc, batch, q, k_pages, v_pages, out, workspace, lse, stream):
+def _attn(call, name, desc, batch, q, k_pages, v_pages, out, workspace, lse, stream, *window):
     n, heads, dim, kind, gpu = batch.n_tokens, desc.heads, desc.head_dim, _kinds.get(desc.dtype), batch.gpu
-    size = 2 * desc.n_pages * desc.kv_heads * desc.page_size * dim
+    size, held = _whole(desc)
     if lse is not None and (lse.shape != (n, heads) or lse.dtype is not _kinds[VQ_F32] or not lse.is_contiguous() or lse.get_device() != gpu):
         raise ValueError(f"{name}: lse is a contiguous float32 tensor [n_tokens, heads] on the batch's GPU")
     if workspace.get_device() != gpu:
         raise ValueError(f"{name}: the workspace is on the batch's GPU")
-    _check(call(desc, batch.struct, q.data_ptr(), _rows(q, n, heads, dim, "q", kind, gpu), _pages(k_pages, size, "k_pages", kind, gpu),
-                _pages(v_pages, size, "v_pages", kind, gpu), out.data_ptr(), _rows(out, n, heads, dim, "out", kind, gpu), _ptr(lse),
+    _check(call(desc, batch.struct, *window, q.data_ptr(), _rows(q, n, heads, dim, "q", kind, gpu), _pages(k_pages, size, "k_pages", held, gpu),
+                _pages(v_pages, size, "v_pages", held, gpu), out.data_ptr(), _rows(out, n, heads, dim, "out", kind, gpu), _ptr(lse),
                 _ptr(workspace), workspace.nbytes, _stream(stream)), name)
 
 
@@ -432,3 +456,13 @@ def vq_attn_decode(desc: VQAttnDesc, batch: AttnBatch, q, k_pages, v_pages, out,
 def vq_attn_prompt(desc: VQAttnDesc, batch: AttnBatch, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:
     """q, out: [n_tokens, heads, head_dim] views (strides as vq_strides allows); lse: float32 [n_tokens, heads] or None."""
     _attn(lib().vq_attn_prompt, "vq_attn_prompt", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream)
+
+
+def vq_attn_decode_window(desc: VQAttnDesc, batch: AttnBatch, window: VQAttnWindow, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:
+    """vq_attn_decode of the window's tokens and the first ones that stay visible."""
+    _attn(lib().vq_attn_decode_window, "vq_attn_decode_window", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream, window)
+
+
+def vq_attn_prompt_window(desc: VQAttnDesc, batch: AttnBatch, window: VQAttnWindow, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:
+    """vq_attn_prompt of each token's window and the first ones that stay visible."""
+    _attn(lib().vq_attn_prompt_window, "vq_attn_prompt_window", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream, window)

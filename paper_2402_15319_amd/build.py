@@ -15,7 +15,9 @@ OBJ_DIR = os.path.join(HERE, "_build")   # object files (kept out of the history
 BENCH_LIB_PATH = os.path.join(HERE, "libvq_bench.so")   # the benchmark's read probe, not part of the product
 BENCH_SOURCES = ["vq_bench_probe.hip"]
 SOURCES = ["vq_api.hip", "vq_pack.hip", "vq_decode.hip", "vq_gemv.hip", "vq_gemv_lora.hip", "vq_gemv_d4.hip", "vq_gemm.hip", "vq_em.hip",
-           "vq_attn_api.hip", "vq_cache.hip", "vq_attn_decode.hip", "vq_attn_prompt.hip", "vq_attn_prompt_256.hip"]
+           "vq_attn_api.hip", "vq_cache.hip", "vq_cache8.hip", "vq_attn_decode.hip", "vq_attn_decode_window.hip", "vq_attn_decode8.hip",
+           "vq_attn_prompt.hip", "vq_attn_prompt_256.hip", "vq_attn_prompt_window.hip", "vq_attn_prompt_window_256.hip", "vq_attn_prompt8.hip",
+           "vq_attn_prompt8_256.hip"]
 # packed-fp32 code generation is switched off on purpose for this machine pool
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
@@ -24,7 +26,8 @@ HIPCC_FLAGS = [
 ]
 # sources with flags of their own: attention keeps its accumulators in vector registers, where it scales them
 ACC_IN_VGPRS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-SOURCE_FLAGS = {"vq_attn_decode.hip": ACC_IN_VGPRS, "vq_attn_prompt.hip": ACC_IN_VGPRS}
+SOURCE_FLAGS = {s: ACC_IN_VGPRS for s in ("vq_attn_decode.hip", "vq_attn_decode_window.hip", "vq_attn_decode8.hip", "vq_attn_prompt.hip",
+                                          "vq_attn_prompt_window.hip", "vq_attn_prompt8.hip")}
 
 
 def _run(cmd, verbose):

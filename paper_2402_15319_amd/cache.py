@@ -1,7 +1,8 @@
 """The pages of a decoder's key-value cache and who holds them: host bookkeeping around vq_cache_copy.
 
 Sequences take pages from one pool as they grow, share them after a fork, give them back when they are freed.  A page that
-several sequences share is copied when one of them writes into it; compaction moves the pages in use to the lowest numbers.
+several sequences share is copied when one of them writes into it; compaction moves the pages in use to the lowest numbers.  Where tokens see a window
+(vq_attn_decode_window), pages that have fallen out of it are given back.
 Buffers, copies and the batches for the attention calls go by the same page numbers in every layer.
 
 Copies are enqueued on the stream given (by default the current one of the cache's GPU): use the cache on one stream, or order the streams.
@@ -13,7 +14,7 @@ import heapq
 
 import torch
 
-from . import VQ_BF16, VQ_F16, AttnBatch, make_attn_desc, vq_cache_copy
+from . import VQ_BF16, VQ_E4M3, VQ_F16, AttnBatch, make_attn_desc, vq_cache_bytes, vq_cache_copy
 
 __all__ = ["PagedCache", "OutOfPages"]
 
@@ -24,19 +25,26 @@ class OutOfPages(RuntimeError):
 
 class PagedCache:
     """layers: how many K and V buffers there are; table_width: pages a sequence may have (its length is at most
-    table_width * page_size).  k[layer] and v[layer] are the buffers, desc the descriptor for the attention calls."""
+    table_width * page_size).  k[layer] and v[layer] are the buffers, desc the descriptor for the attention calls.  cache_dtype: VQ_E4M3 for pages in
+    8 bits (the buffers are then flat uint8 tensors), None for pages of dtype."""
 
     def __init__(self, layers: int, heads: int, kv_heads: int, head_dim: int, page_size: int, n_pages: int, table_width: int,
-                 dtype: int = VQ_F16, scale: float | None = None, device="cuda:0"):
+                 dtype: int = VQ_F16, scale: float | None = None, device="cuda:0", cache_dtype: int | None = None):
         if layers < 1 or n_pages < 1 or table_width < 1:
             raise ValueError("PagedCache: layers, n_pages and table_width are positive")
         if dtype not in (VQ_F16, VQ_BF16):
             raise ValueError("PagedCache: dtype is VQ_F16 or VQ_BF16")
-        self.desc = make_attn_desc(heads, kv_heads, head_dim, page_size, n_pages, dtype, scale)
+        if cache_dtype not in (None, VQ_E4M3):
+            raise ValueError("PagedCache: cache_dtype is VQ_E4M3 or None")
+        self.desc = make_attn_desc(heads, kv_heads, head_dim, page_size, n_pages, dtype, scale, cache_dtype)
         self.page_size, self.n_pages, self.table_width, self.device = page_size, n_pages, table_width, device
-        kind = torch.float16 if dtype == VQ_F16 else torch.bfloat16
-        self.k = [torch.empty(n_pages, kv_heads, page_size, head_dim, dtype=kind, device=device) for _ in range(layers)]
-        self.v = [torch.empty(n_pages, kv_heads, head_dim, page_size, dtype=kind, device=device) for _ in range(layers)]
+        if cache_dtype is None:
+            kind = torch.float16 if dtype == VQ_F16 else torch.bfloat16
+            self.k = [torch.empty(n_pages, kv_heads, page_size, head_dim, dtype=kind, device=device) for _ in range(layers)]
+            self.v = [torch.empty(n_pages, kv_heads, head_dim, page_size, dtype=kind, device=device) for _ in range(layers)]
+        else:
+            size = vq_cache_bytes(self.desc)
+            self.k, self.v = ([torch.empty(size, dtype=torch.uint8, device=device) for _ in range(layers)] for _ in "kv")
         self._buffers = self.k + self.v
         self._free = list(range(n_pages))   # a heap: the lowest numbers are given out first
         self._holders = [0] * n_pages       # sequences that list a page
@@ -56,6 +64,7 @@ class PagedCache:
         return self._length[s]
 
     def pages(self, s: int) -> list[int]:
+        """The pages of s in the order of its tokens; -1 for one that was given back."""
         return list(self._pages[s])
 
     @property
@@ -68,16 +77,41 @@ class PagedCache:
         t = self.add()
         self._pages[t], self._length[t] = pages, length
         for p in self._pages[t]:
-            self._holders[p] += 1
+            if p >= 0:
+                self._holders[p] += 1
         return t
 
     def free(self, s: int) -> None:
         """Forgets s; pages that nobody else holds go back to the pool."""
         for p in self._pages.pop(s):
-            self._holders[p] -= 1
-            if self._holders[p] == 0:
-                heapq.heappush(self._free, p)
+            self._release(p)
         del self._length[s]
+
+    def slide(self, sequences, window: int, sinks: int = 0) -> int:
+        """Forgets the tokens that no token to come sees: of every sequence those but the last window - 1 and the first `sinks`, in whole
+        pages; how many pages the sequences gave back (a page goes back to the pool when nobody holds it).  Rows that are already in the cache no
+        longer see all of their window after this: call it behind their attention, with the largest window and sinks that are used."""
+        if window < 1 or sinks < 0:
+            raise ValueError("slide: window is positive, sinks not negative")
+        sequences = list(sequences)
+        for s in sequences:
+            self._pages[s]   # all are there before anything changes
+        given = 0
+        for s in sequences:
+            own = self._pages[s]
+            for j in range(-(-sinks // self.page_size), max(0, self._length[s] - window + 1) // self.page_size):
+                if own[j] >= 0:
+                    self._release(own[j])
+                    own[j] = -1
+                    given += 1
+        return given
+
+    def _release(self, page: int) -> None:
+        if page < 0:
+            return
+        self._holders[page] -= 1
+        if self._holders[page] == 0:
+            heapq.heappush(self._free, page)
 
     def grow(self, sequences, new, stream=None) -> None:
         """Room for new[i] more tokens in sequences[i] (each named once); their lengths count them from here on.  A last page

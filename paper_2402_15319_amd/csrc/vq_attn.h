@@ -28,7 +28,11 @@ struct AppendArgs {
   uint16_t* k_pages;
   uint16_t* v_pages;
   Strides ks, vs;
+  float* k_scales;     // pages in 8 bits: [page][kv head][block]; NULL: pages in 16 bits
+  float* v_scales;
+  int32_t bf16;        // the type of k and v: bf16, or fp16
 };
+constexpr int kBlock = 16;   // slots of a head that share a scale
 
 struct AttnArgs {
   CacheArgs c;
@@ -40,7 +44,11 @@ struct AttnArgs {
   Strides qs, os;
   int32_t heads, group;   // group: query heads that share a key/value head
   float scale_log2;    // scale * log2(e): the kernels work with powers of two
+  int32_t window, sinks;    // window 0: every token up to a row's own is seen
+  const float* k_scales;    // pages in 8 bits: [page][kv head][block of 16 slots]; NULL: pages in 16 bits
+  const float* v_scales;
 };
+constexpr int kEveryToken = 1 << 30;   // a window that no sequence reaches the end of
 
 // How a call of vq_attn_decode is split: a workgroup takes `chunk` tokens of one sequence and up to 16 query heads of one
 // key/value head (a tile); where a sequence has several parts, the last of their workgroups to finish joins them.
@@ -52,6 +60,7 @@ struct DecodePlan {
 };
 constexpr int kJoinCounters = 16384;   // at the start of the workspace: parts that have finished, zero between calls
 constexpr int kTileHeads = 16, kTogetherDim = 128;   // several tiles up to this head_dim: two of larger ones do not fit the registers (three of 128 spill 80 bytes)
+constexpr int kThreeDim8 = 64;         // three tiles in 8 bits up to this head_dim: of 96 and 128 they spill 36 and 252 bytes
 constexpr int kMostParts = 64;         // of a sequence
 
 struct DecodeArgs {
@@ -89,7 +98,8 @@ constexpr int kCopyBuffers = 128, kCopyPairs = 1024, kCopyFew = 64;
 template <int PAIRS>
 struct CopyArgsOf {
   uint64_t page_bytes;
-  int32_t n_buffers, n_pairs, pieces, reserved;   // pieces: workgroups for a page
+  uint64_t scales_at;   // bytes from the first page to its scales, of which a page has scale_words
+  int32_t n_buffers, n_pairs, pieces, scale_words;   // pieces: workgroups for a page
   void* buffer[kCopyBuffers];
   int32_t from_to[PAIRS][2];
 };
@@ -97,9 +107,16 @@ typedef CopyArgsOf<kCopyPairs> CopyArgs;
 static_assert(sizeof(CopyArgs) <= 16384, "kernel arguments");
 
 hipError_t launch_append(const AppendArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_append8(const AppendArgs& a, int head_dim, hipStream_t s);   // pages in 8 bits
 hipError_t launch_copy(CopyArgs& a, hipStream_t s);
 hipError_t launch_attn_decode(const DecodeArgs& a, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_attn_decode_window(const DecodeArgs& a, int head_dim, bool bf16, hipStream_t s);   // pages in 16 bits
+hipError_t launch_attn_decode8(const DecodeArgs& a, int head_dim, bool bf16, hipStream_t s);         // pages in 8 bits, a.window as it is
 hipError_t launch_attn_prompt(const PromptArgs& a, int head_dim, bool bf16, hipStream_t s);
 hipError_t launch_attn_prompt_256(const PromptArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_attn_prompt_window(const PromptArgs& a, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_attn_prompt_window_256(const PromptArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_attn_prompt8(const PromptArgs& a, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_attn_prompt8_256(const PromptArgs& a, bool bf16, hipStream_t s);
 
 }  // namespace vq

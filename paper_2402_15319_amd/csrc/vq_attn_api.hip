@@ -17,7 +17,7 @@ constexpr float kLog2E = 1.44269504088896f;
 
 int check_attn_desc(const vq_attn_desc* d, bool scaled) {
   if (!d) return VQ_ERR_NULL;
-  if (d->heads < 1 || d->kv_heads < 1 || d->head_dim < 1 || d->page_size < 1 || d->n_pages < 1 || d->reserved != 0) return VQ_ERR_BAD_DESC;
+  if (d->heads < 1 || d->kv_heads < 1 || d->head_dim < 1 || d->page_size < 1 || d->n_pages < 1 || (d->cache_dtype != 0 && d->cache_dtype != VQ_E4M3)) return VQ_ERR_BAD_DESC;
   if (d->heads % d->kv_heads != 0) return VQ_ERR_BAD_DESC;
   if (d->heads > 1024) return VQ_ERR_UNSUPPORTED;
   if (d->head_dim != 64 && d->head_dim != 96 && d->head_dim != 128 && d->head_dim != 256) return VQ_ERR_UNSUPPORTED;
@@ -25,6 +25,14 @@ int check_attn_desc(const vq_attn_desc* d, bool scaled) {
   if (d->dtype != VQ_F16 && d->dtype != VQ_BF16) return VQ_ERR_UNSUPPORTED;
   if (scaled && !(d->scale > 0.f && d->scale * kLog2E <= 3.402823466e38f)) return VQ_ERR_BAD_ARG;   // a NaN fails both
   return VQ_OK;
+}
+
+// Bytes of the codes, or values, of a page, and of its scales.
+bool eight_bits(const vq_attn_desc& d) { return d.cache_dtype == VQ_E4M3; }
+int64_t page_bytes(const vq_attn_desc& d) { return (int64_t)d.kv_heads * d.page_size * d.head_dim * (eight_bits(d) ? 1 : 2); }
+int64_t scale_bytes(const vq_attn_desc& d) { return eight_bits(d) ? (int64_t)d.kv_heads * (d.page_size / kBlock) * 4 : 0; }
+const float* scales_of(const vq_attn_desc& d, const void* pages) {
+  return eight_bits(d) ? (const float*)((const char*)pages + d.n_pages * page_bytes(d)) : nullptr;
 }
 
 constexpr int kMostLen = 1 << 29;   // tokens of a sequence: the kernels' token indexes stay within 32 bits with room to spare
@@ -94,32 +102,49 @@ bool aligned_rows(const void* p, const Strides& s) {
   return s.dim == 1 && ((s.token | s.head) & 7) == 0 ? aligned16(p) : ((uintptr_t)p & 1) == 0;
 }
 
-constexpr int kPartStep = 128;            // tokens that a workgroup takes at a time
+constexpr int kPartStep = 128;            // tokens that a workgroup takes at a time, of pages in 16 bits
+int part_step(const vq_attn_desc& d) { return eight_bits(d) ? 2 * kPartStep : kPartStep; }
 // Workgroups: one for each CU.  The plans count on 256 CUs rather than on the device's: they follow from sizes alone, so that a
 // workspace can be asked for without a device.
 constexpr int64_t kEnoughUnits = 256;
 constexpr int64_t kTogetherUnits = 16;
 constexpr int kLongPart = 4096, kShortPart = 1024;
 constexpr int kShortValues = 32768;       // of a sequence's keys: no parts up to here
+int most_together(const vq_attn_desc& d) { return eight_bits(d) && d.head_dim > kThreeDim8 ? 2 : 3; }
+
+// What of a sequence of max_len tokens a new one goes through: the sinks and the window, to whole steps of a wave.
+int64_t decode_seen(const vq_attn_desc& d, int64_t max_len, const vq_attn_window* w) {
+  if (!w) return max_len;
+  const int64_t step = part_step(d) / 4, seen = (w->sinks + step - 1) / step * step + w->window + step;
+  return seen < max_len ? seen : max_len;
+}
+
+// The same for the new tokens of a tile, of which there are up to kPromptRows, in steps of kPromptTokens.
+int64_t prompt_seen(int64_t max_len, const vq_attn_window* w) {
+  if (!w) return max_len;
+  const int64_t seen = (w->sinks + (int64_t)kPromptTokens - 1) / kPromptTokens * kPromptTokens + w->window + kPromptRows + 2 * kPromptTokens;
+  return seen < max_len ? seen : max_len;
+}
 
 DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   DecodePlan p;
   const int group = d.heads / d.kv_heads;
   p.tiles = (group + kTileHeads - 1) / kTileHeads;
   p.cols = group < kTileHeads ? group : kTileHeads;
-  p.together = d.head_dim > kTogetherDim || p.tiles == 1 ? 1 : p.tiles == 2 || p.tiles == 4 ? 2 : 3;
+  p.together = d.head_dim > kTogetherDim || p.tiles == 1 ? 1 : p.tiles == 2 || p.tiles == 4 ? 2 : most_together(d);
   // Three tiles together read a key/value head once, but leave one workgroup to join all of their parts: with 48 heads to one of 128 and
   // sequences of 4,096 to 8,192, 64 of them take 59 us (a tile to a workgroup 118) and 32 36 (76); with fewer the join is longer than what
   // it saves (16 46 us and 43, 8 50 and 28).
   if ((int64_t)b.n_seqs * d.kv_heads * ((p.tiles + p.together - 1) / p.together) < kTogetherUnits) p.together = 1;
   const int64_t units = (int64_t)b.n_seqs * d.kv_heads * ((p.tiles + p.together - 1) / p.together);
-  const int64_t steps = b.max_len > kPartStep ? ((int64_t)b.max_len + kPartStep - 1) / kPartStep : 1;
+  const int step = part_step(d);
+  const int64_t steps = b.max_len > step ? ((int64_t)b.max_len + step - 1) / step : 1;
   int64_t parts = 1;
   p.waves = 4;
   if ((int64_t)b.max_len * d.head_dim <= kShortValues) {
     // One part of 8 waves: a step or two for each of them cost less than the join (a sequence of 256 tokens x 32 heads of 128 6.1
     // us, in two parts of 4 waves 7.7; of 512 8.9 and 8.0; of 512 x 32 heads of 64 5.6 and 7.7).
-    p.waves = b.max_len > 32 * p.waves && p.together == 1 ? 8 : 4;
+    p.waves = b.max_len > step && p.together == 1 ? 8 : 4;
   } else if (units * p.together <= kJoinCounters) {
     // Fewer workgroups than CUs: as many parts as fill the chip once, up to 4,096 tokens each (130,001 tokens x 8 heads: 256
     // workgroups 97 us, 512 100, 1,024 106).  As many without a split: parts of 1,024 tokens, which even out what the lengths differ
@@ -127,14 +152,14 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
     // 177).  Lengths can differ in the first case too, and only max_len is known here: 31 sequences of 1 to 8,192 x 8 heads have two
     // parts each and take 50 us, 32 of them eight and 58.
     const int64_t most = units < kEnoughUnits ? kLongPart : kShortPart;
-    const int64_t enough = (kEnoughUnits + units - 1) / units, least = (steps * kPartStep + most - 1) / most;
+    const int64_t enough = (kEnoughUnits + units - 1) / units, least = (steps * step + most - 1) / most;
     parts = (least + enough - 1) / enough * enough;   // as many for every CU
     parts = parts < kMostParts ? parts : kMostParts;
     parts = parts < steps ? parts : steps;
   }
   const int64_t per = (steps + parts - 1) / parts;   // steps of a part
   p.parts = (int32_t)((steps + per - 1) / per);
-  p.chunk = (int32_t)(per * kPartStep);
+  p.chunk = (int32_t)(per * step);
   return p;
 }
 
@@ -193,14 +218,14 @@ int64_t decode_most_parts(const vq_attn_desc& d, int64_t n_seqs, int64_t max_len
   b.max_len = 1;
   const DecodePlan p = decode_plan(d, b);
   const auto least = [](int64_t tokens) { return tokens < 1 ? 1 : tokens; };
-  const int64_t steps = (max_len + kPartStep - 1) / kPartStep, most = steps < kMostParts ? steps : kMostParts;
+  const int64_t step = part_step(d), steps = (max_len + step - 1) / step, most = steps < kMostParts ? steps : kMostParts;
   const int64_t wide = d.kv_heads * (int64_t)((p.tiles + p.together - 1) / p.together), tiles = n_seqs * d.kv_heads * p.tiles;
   // Fewer than kEnoughUnits units: parts of kLongPart tokens, and up to kEnoughUnits / units - 1 more for as many on every CU.
   const int64_t few = tiles < (kEnoughUnits - 1) * p.together ? tiles : (kEnoughUnits - 1) * p.together;
-  const int64_t by_length = few * least((steps * kPartStep + kLongPart - 1) / kLongPart) + (kEnoughUnits - 1) * p.together;
+  const int64_t by_length = few * least((steps * step + kLongPart - 1) / kLongPart) + (kEnoughUnits - 1) * p.together;
   int64_t parts = few * most < by_length ? few * most : by_length;
   if (n_seqs * wide >= kEnoughUnits) {
-    const int64_t many = tiles < kJoinCounters ? tiles : kJoinCounters, each = least((steps * kPartStep + kShortPart - 1) / kShortPart);
+    const int64_t many = tiles < kJoinCounters ? tiles : kJoinCounters, each = least((steps * step + kShortPart - 1) / kShortPart);
     const int64_t of_many = many * (each < most ? each : most);
     parts = of_many > parts ? of_many : parts;
   }
@@ -232,13 +257,14 @@ size_t workspace(const vq_attn_desc& d, const vq_attn_batch& b) {
   return (kJoinCounters + (of_decode > of_prompt ? of_decode : of_prompt)) * sizeof(float);
 }
 
-int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,
+int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const vq_attn_window* window, const void* q, const vq_strides* q_strides, const void* k_pages,
               const void* v_pages, void* out, const vq_strides* out_strides, float* lse_f32, void* workspace, size_t workspace_bytes,
               void* stream, bool decode) {
   int st = check_attn_desc(desc, true);
   if (st != VQ_OK) return st;
   st = check_batch(*desc, batch, decode);
   if (st != VQ_OK) return st;
+  if (window && (window->window < 1 || window->window > kMostLen || window->sinks < 0 || window->sinks > kMostLen)) return VQ_ERR_BAD_ARG;
   if (!q || !k_pages || !v_pages || !out || !workspace) return VQ_ERR_NULL;
   if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(workspace) || !aligned4(lse_f32)) return VQ_ERR_ALIGN;
   if (q == out || k_pages == out || v_pages == out) return VQ_ERR_BAD_ARG;
@@ -259,12 +285,19 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* 
   a.heads = desc->heads;
   a.group = desc->heads / desc->kv_heads;
   a.scale_log2 = desc->scale * kLog2E;
+  a.window = window ? window->window : eight_bits(*desc) ? kEveryToken : 0;   // the kernels of pages in 8 bits all look at it
+  a.sinks = window ? window->sinks : 0;
+  a.k_scales = scales_of(*desc, k_pages);
+  a.v_scales = scales_of(*desc, v_pages);
+  // A window bounds what is gone through; the plan is that of sequences of such lengths, whose workspace is no larger.
+  vq_attn_batch seen = *batch;
+  seen.max_len = (int32_t)(decode ? decode_seen(*desc, batch->max_len, window) : prompt_seen(batch->max_len, window));
   const bool bf16 = desc->dtype == VQ_BF16;
   if (!decode) {
-    const PromptArgs prompt = {a, prompt_plan(*desc, *batch), (uint32_t*)workspace, (float*)workspace + kJoinCounters};
+    const PromptArgs prompt = {a, prompt_plan(*desc, seen), (uint32_t*)workspace, (float*)workspace + kJoinCounters};
     return hip_status(launch_attn_prompt(prompt, desc->head_dim, bf16, (hipStream_t)stream));
   }
-  both.plan = decode_plan(*desc, *batch);
+  both.plan = decode_plan(*desc, seen);
   both.counter = (uint32_t*)workspace;
   both.part = (float*)workspace + kJoinCounters;
   return hip_status(launch_attn_decode(both, desc->head_dim, bf16, (hipStream_t)stream));
@@ -281,7 +314,7 @@ int vq_cache_bytes(const vq_attn_desc* desc, size_t* bytes) {
   const int st = check_attn_desc(desc, false);
   if (st != VQ_OK) return st;
   if (!bytes) return VQ_ERR_NULL;
-  *bytes = (size_t)desc->n_pages * desc->kv_heads * desc->page_size * desc->head_dim * 2;
+  *bytes = (size_t)desc->n_pages * (size_t)(page_bytes(*desc) + scale_bytes(*desc));
   return VQ_OK;
 }
 
@@ -305,6 +338,9 @@ int vq_cache_append(const vq_attn_desc* desc, const vq_attn_batch* batch, const 
   a.v = (const uint16_t*)v;
   a.k_pages = (uint16_t*)k_pages;
   a.v_pages = (uint16_t*)v_pages;
+  a.k_scales = (float*)scales_of(*desc, k_pages);
+  a.v_scales = (float*)scales_of(*desc, v_pages);
+  a.bf16 = desc->dtype == VQ_BF16;
   return hip_status(launch_append(a, desc->head_dim, (hipStream_t)stream));
 }
 
@@ -324,8 +360,9 @@ int vq_cache_copy(const vq_attn_desc* desc, int n_buffers, void* const* buffers,
   constexpr int kSlots = 4096;
   static_assert(kSlots >= 4 * kCopyPairs, "half full at most");
   CopyArgs a;
-  a.reserved = 0;
-  a.page_bytes = (uint64_t)desc->kv_heads * desc->page_size * desc->head_dim * 2;
+  a.page_bytes = (uint64_t)page_bytes(*desc);
+  a.scale_words = (int32_t)(scale_bytes(*desc) / 4);
+  a.scales_at = (uint64_t)desc->n_pages * a.page_bytes;
   for (int first = 0; first < n_pairs;) {
     int32_t page[kSlots];
     uint8_t use[kSlots];
@@ -375,13 +412,27 @@ int vq_attn_workspace_bytes(const vq_attn_desc* desc, const vq_attn_batch* batch
 int vq_attn_decode(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,
                    const void* v_pages, void* out, const vq_strides* out_strides, float* lse_f32, void* workspace, size_t workspace_bytes,
                    void* stream) {
-  return attn_impl(desc, batch, q, q_strides, k_pages, v_pages, out, out_strides, lse_f32, workspace, workspace_bytes, stream, true);
+  return attn_impl(desc, batch, nullptr, q, q_strides, k_pages, v_pages, out, out_strides, lse_f32, workspace, workspace_bytes, stream, true);
 }
 
 int vq_attn_prompt(const vq_attn_desc* desc, const vq_attn_batch* batch, const void* q, const vq_strides* q_strides, const void* k_pages,
                    const void* v_pages, void* out, const vq_strides* out_strides, float* lse_f32, void* workspace, size_t workspace_bytes,
                    void* stream) {
-  return attn_impl(desc, batch, q, q_strides, k_pages, v_pages, out, out_strides, lse_f32, workspace, workspace_bytes, stream, false);
+  return attn_impl(desc, batch, nullptr, q, q_strides, k_pages, v_pages, out, out_strides, lse_f32, workspace, workspace_bytes, stream, false);
+}
+
+int vq_attn_decode_window(const vq_attn_desc* desc, const vq_attn_batch* batch, const vq_attn_window* window, const void* q,
+                          const vq_strides* q_strides, const void* k_pages, const void* v_pages, void* out, const vq_strides* out_strides,
+                          float* lse_f32, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!window) return VQ_ERR_NULL;
+  return attn_impl(desc, batch, window, q, q_strides, k_pages, v_pages, out, out_strides, lse_f32, workspace, workspace_bytes, stream, true);
+}
+
+int vq_attn_prompt_window(const vq_attn_desc* desc, const vq_attn_batch* batch, const vq_attn_window* window, const void* q,
+                          const vq_strides* q_strides, const void* k_pages, const void* v_pages, void* out, const vq_strides* out_strides,
+                          float* lse_f32, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!window) return VQ_ERR_NULL;
+  return attn_impl(desc, batch, window, q, q_strides, k_pages, v_pages, out, out_strides, lse_f32, workspace, workspace_bytes, stream, false);
 }
 
 }  // extern "C"

@@ -95,6 +95,22 @@ template <bool BF16> __device__ __forceinline__ u32x4 pack8(f32x8 p) {
   else return __builtin_bit_cast(u32x4, __builtin_convertvector(p, f16x8));
 }
 
+// Eight codes (e4m3, two dwords) as values of the cache's type: exactly, for a block's scale is a power of two that leaves every code a
+// number of the type.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <bool BF16> __device__ __forceinline__ u32x4 values8(uint32_t lo, uint32_t hi, float scale) {
+  if constexpr (BF16)
+    return {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+  else
+    return {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true))};
+}
+
 // What one workgroup hands to another of the same launch goes past the caches that only some of the XCDs see: accesses of agent
 // scope, two values at a time, and before the word that says so the stores' completion.  (Fences of agent scope would do the
 // same for ordinary accesses, but write back and drop the XCD's whole L2: 24 sequences of 2,000 to 4,096 tokens in two parts, 1,536
@@ -118,6 +134,9 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t voff, uin
 __device__ __forceinline__ void lds_turn() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
+
+// The same where nothing comes into LDS past the registers: the wave's writes to LDS and reads from it are done, its loads stay under way.
+__device__ __forceinline__ void lds_written() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp
 

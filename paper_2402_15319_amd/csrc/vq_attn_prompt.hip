@@ -1,21 +1,26 @@
-// Causal attention of prompts: heads of 64, 96 and 128.
+// Causal attention of prompts: pages in 16 bits, every earlier token, heads of 64, 96 and 128.
 #include "vq_attn_prompt_impl.h"
 
 namespace vq {
 namespace {
 
-template <bool BF16>
-hipError_t launch_type(const PromptArgs& a, int head_dim, hipStream_t s) {
-  if (head_dim == 64) return launch_prompt<BF16, 64>(a, s);
-  if (head_dim == 96) return launch_prompt<BF16, 96>(a, s);
-  return launch_prompt<BF16, 128>(a, s);
+template <bool BF16, int D, int TEAMS>
+__global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_kernel(const PromptArgs A) {
+  prompt_body<BF16, D, TEAMS, false, false>(A);
 }
+
+struct Kernels {
+  template <bool BF16, int D, int TEAMS>
+  static constexpr auto kernel = prompt_kernel<BF16, D, TEAMS>;
+};
 
 }  // namespace
 
 hipError_t launch_attn_prompt(const PromptArgs& a, int head_dim, bool bf16, hipStream_t s) {
+  if (a.a.k_scales) return launch_attn_prompt8(a, head_dim, bf16, s);
+  if (a.a.window > 0) return launch_attn_prompt_window(a, head_dim, bf16, s);
   if (head_dim == 256) return launch_attn_prompt_256(a, bf16, s);
-  return bf16 ? launch_type<true>(a, head_dim, s) : launch_type<false>(a, head_dim, s);
+  return bf16 ? launch_prompt_small<Kernels, true>(a, head_dim, s) : launch_prompt_small<Kernels, false>(a, head_dim, s);
 }
 
 }  // namespace vq

@@ -1,4 +1,4 @@
-// Causal attention of any number of new tokens of every sequence over the paged cache: the kernel.
+// Causal attention of any number of new tokens of every sequence over the paged cache: the kernels' body.
 #pragma once
 #include <type_traits>
 
@@ -23,8 +23,12 @@ template <int D> __device__ __forceinline__ int k_turn(int r) {
 //   it is: row m of the first operand is token m with bits 2 and 3 exchanged, which leaves a lane with eight successive tokens.
 // K and V^T of a step come into LDS past the registers, each wave 16 tokens of both (one page), while the step before is
 // worked on.  With two teams of such waves (see the plan) each takes every second step, and the second's sums go to the first in the end.
-template <bool BF16, int D, int TEAMS>
-__global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_kernel(const PromptArgs A) {
+// E4M3: pages in 8 bits.  A wave's 16 tokens are one block; their codes come into registers while the step before the one before is worked on, and go
+// to LDS as values of the type (exactly), each once for the workgroup, so that the products are those of 16 bits.
+// WINDOW: a.window and a.sinks.  What no row of the tile sees between the sinks and the window, in whole steps, is passed over: `step` counts the
+// steps that are gone through, real(step) is the place of one in the sequence.
+template <bool BF16, int D, int TEAMS, bool E4M3, bool WINDOW>
+__device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   const AttnArgs& a = A.a;
   constexpr int KS = D / 16, DT = D / 32, kLoads = D / 32;     // loads of a wave for its 16 tokens' K, and for their V
   constexpr int kHalf = kTokens * D * 2, kStep = 2 * kHalf;    // bytes of K, or V, of a step
@@ -51,7 +55,16 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
   const bool valid = row + col <= end && token_in < n;
   const int most = behind + (token0 + tokens < n ? token0 + tokens : n) - 1;   // highest position of the tile
   const int pos = behind + token, wave_first = behind + low, wave_last = low < n ? behind + high : -1;
-  const int all = most < 0 ? 0 : most / kTokens + 1;       // steps of the tile, and this part's: begin .. steps - 1
+  // The first token in a window of the tile; steps sink_steps .. sink_steps + skip - 1 are passed over.
+  int first_seen = 0, sink_steps = 0, skip = 0;
+  if constexpr (WINDOW) {
+    first_seen = behind + token0 - a.window + 1 > 0 ? behind + token0 - a.window + 1 : 0;
+    sink_steps = a.sinks < first_seen ? (a.sinks + kTokens - 1) / kTokens : first_seen / kTokens;
+    skip = first_seen / kTokens - sink_steps;
+    skip = skip > 0 ? skip : 0;
+  }
+  auto real = [&](int step) { return WINDOW && step >= sink_steps ? step + skip : step; };
+  const int all = most < 0 ? 0 : most / kTokens + 1 - skip;   // steps of the tile, and this part's: begin .. steps - 1
   const int begin = blockIdx.y * A.plan.steps, steps = all - begin < A.plan.steps ? all : begin + A.plan.steps;
   if (begin >= all && begin > 0) return;
 
@@ -59,17 +72,19 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
   // pieces of eight tokens, exchanged where bit 3 of the dimension is set.
   const int shift = a.c.page_shift, mask = (1 << shift) - 1, last_page = len > 0 ? (len - 1) >> shift : 0;
   uint32_t k_off[kLoads];
+  if constexpr (!E4M3) {
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) {
-    const int at = 64 * j + lane, r = at / (D / 8), p = at % (D / 8);
-    k_off[j] = (r * D + (p ^ k_turn<D>(r)) * 8) * 2;
+    for (int j = 0; j < kLoads; ++j) {
+      const int at = 64 * j + lane, r = at / (D / 8), p = at % (D / 8);
+      k_off[j] = (r * D + (p ^ k_turn<D>(r)) * 8) * 2;
+    }
   }
   const uint32_t v_off = (((lane >> 1) << shift) + 8 * ((lane & 1) ^ ((lane >> 4) & 1))) * 2;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds) + team * (2 * kStep);
   const int32_t* table = a.c.table + (int64_t)s * a.c.table_width;
   // Lane i: the wave's page in the i-th (mod 64) of the steps that are being loaded; asked for before q, which the loads need not wait for.
   auto pages_from = [&](int step) {
-    const int j = ((step + TEAMS * lane) * kTokens + 16 * wave) >> shift;
+    const int j = (real(step + TEAMS * lane) * kTokens + 16 * wave) >> shift;
     return table[j < last_page ? j : last_page];
   };
   int pages = pages_from(begin + team);
@@ -85,11 +100,14 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
     }
   }
 
-  auto load = [&](int step) {
+  auto page_of = [&](int step) {   // of the wave's tokens; steps one after another
     const int at = ((step - begin) / TEAMS) & 63;
     if (at == 0 && step >= begin + TEAMS) pages = pages_from(step);
-    const int page = page_inside(a.c, __builtin_amdgcn_readlane(pages, at));
-    const int in = (step * kTokens + 16 * wave) & mask;
+    return page_inside(a.c, __builtin_amdgcn_readlane(pages, at));
+  };
+  auto load = [&](int step) {
+    const int page = page_of(step);
+    const int in = (real(step) * kTokens + 16 * wave) & mask;
     const int64_t page_head = ((int64_t)page * a.c.kv_heads + kvh) * ((int64_t)D << shift);
     const uint16_t* k = a.k_pages + page_head + in * D;
     const uint16_t* v = a.v_pages + page_head + in;
@@ -99,9 +117,70 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) load_to_lds(v + ((int64_t)(32 * j) << shift), v_off, to + kHalf + 1024 * j);
   };
+  // The same in 8 bits, in two halves.  16 codes of a token's dimensions, or of a dimension's tokens, to a load; of heads of 96 the last 32 dimensions
+  // are 8 to a load.
+  constexpr int kCodes = D / 64, kFrags = (D + 63) / 64;
+  u32x4 k_codes[E4M3 ? kFrags : 1], v_codes[E4M3 ? kFrags : 1];
+  float k_scale = 1.f, v_scale = 1.f;
+  auto here = [&]() {   // the lane, from which the places below are made again in every step: kept, they would take registers of the products
+    int x = lane;
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  auto fetch = [&](int step) {
+    const int lane = here();
+    const int page = page_of(step);
+    const int in = (real(step) * kTokens + 16 * wave) & mask;
+    const int64_t head = (int64_t)page * a.c.kv_heads + kvh;
+    const uint8_t* k = reinterpret_cast<const uint8_t*>(a.k_pages) + (head * D << shift) + in * D;
+    const uint8_t* v = reinterpret_cast<const uint8_t*>(a.v_pages) + (head * D << shift) + in;
+    const int64_t block = (head << (shift - 4)) + (in >> 4);
+    k_scale = a.k_scales[block];
+    v_scale = a.v_scales[block];
+#pragma unroll
+    for (int j = 0; j < kCodes; ++j) {
+      k_codes[j] = *reinterpret_cast<const u32x4*>(k + 1024 * j + 16 * lane);
+      v_codes[j] = *reinterpret_cast<const u32x4*>(v + ((64 * j + lane) << shift));
+    }
+    if constexpr (E4M3 && kFrags > kCodes) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(k + 1024 * kCodes + 8 * lane);
+      const u32x2 y = *reinterpret_cast<const u32x2*>(v + ((64 * kCodes + (lane >> 1)) << shift) + 8 * (lane & 1));
+      k_codes[kCodes] = {x[0], x[1], 0, 0};
+      v_codes[kCodes] = {y[0], y[1], 0, 0};
+    }
+  };
+  auto store = [&](int step) {
+    const int lane = here();
+    char* to = lds + (2 * team + ((step / TEAMS) & 1)) * kStep + wave * (kHalf / kWaves);
+    auto k_piece = [&](int at, u32x4 v) {   // of 8 dimensions: the at-th of the wave's tokens, one token after another
+      const int r = at / (D / 8), p = at % (D / 8);
+      *reinterpret_cast<u32x4*>(to + (r * (D / 8) + (p ^ k_turn<D>(r))) * 16) = v;
+    };
+    auto v_piece = [&](int d, int h, u32x4 v) { *reinterpret_cast<u32x4*>(to + kHalf + (2 * d + (h ^ ((d >> 3) & 1))) * 16) = v; };
+#pragma unroll
+    for (int j = 0; j < kCodes; ++j) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        k_piece(128 * j + 2 * lane + h, values8<BF16>(k_codes[j][2 * h], k_codes[j][2 * h + 1], k_scale));
+        v_piece(64 * j + lane, h, values8<BF16>(v_codes[j][2 * h], v_codes[j][2 * h + 1], v_scale));
+      }
+    }
+    if constexpr (E4M3 && kFrags > kCodes) {
+      k_piece(128 * kCodes + lane, values8<BF16>(k_codes[kCodes][0], k_codes[kCodes][1], k_scale));
+      v_piece(64 * kCodes + (lane >> 1), lane & 1, values8<BF16>(v_codes[kCodes][0], v_codes[kCodes][1], v_scale));
+    }
+  };
 
   int step = begin + team;
-  if (step < steps) load(step);
+  if constexpr (E4M3) {
+    if (step < steps) {
+      fetch(step);
+      store(step);
+      if (step + TEAMS < steps) fetch(step + TEAMS);
+    }
+  } else {
+    if (step < steps) load(step);
+  }
 #pragma unroll
   for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));   // here, or the compiler waits for them in the loop, and with them for its loads
 
@@ -113,16 +192,18 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   const int k_row = (col & 0x13) | (col & 4) << 1 | (col & 8) >> 1;
   uint32_t left_out = 0;   // values that are no numbers, in steps with a mask
-  auto up_to_last = [&](int at) {   // what is left of the lane's tokens at + 8 half .. + 7: those up to the sequence's last one
-    const int rest = len - at - 8 * half;
+  auto up_to_last = [&](int at) {   // what is left of the lane's tokens at + 8 half .. + 7: those up to the sequence's last one that some row may see
+    const int rest = len - at - 8 * half, lo = WINDOW ? a.sinks - at - 8 * half : 0, hi = WINDOW ? first_seen - at - 8 * half : 0;
+    auto there = [&](int i) { return i < rest && (!WINDOW || i < lo || i >= hi); };
     u32x4 keep;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) keep[j] = (2 * j < rest ? 0xffffu : 0u) | (2 * j + 1 < rest ? 0xffff0000u : 0u);
+    for (int j = 0; j < 4; ++j) keep[j] = (there(2 * j) ? 0xffffu : 0u) | (there(2 * j + 1) ? 0xffff0000u : 0u);
     return keep;
   };
 
-  auto work = [&](int step, auto masked_) {
-    constexpr bool masked = decltype(masked_)::value;
+  // masked: some row of the wave leaves out some token of the step.  Where it is known only here (WINDOW), both kinds of steps are one stretch of code.
+  auto work = [&](int step, auto masked) {
+    constexpr bool known = !std::is_same<decltype(masked), bool>::value;
     const char* kt = lds + (2 * team + ((step / TEAMS) & 1)) * kStep;
     const char* vt = kt + kHalf;
     f32x16 x[2];
@@ -153,14 +234,18 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
       for (int j = 0; j < kBatch; ++j) f[j] = *reinterpret_cast<const u32x4*>(v_at + ((at + j) / DT * D + (at + j) % DT * 32) * 32);
       __builtin_amdgcn_sched_barrier(0);
     };
-    if constexpr (!masked) v_batch(0);   // under way while the weights are made
+    if (!known || !masked) v_batch(0);   // under way while the weights are made
     __builtin_amdgcn_s_setprio(0);
-    const int rel = pos - step * kTokens - 8 * half;   // tokens of the lane up to here are attended
-    if constexpr (masked) {
+    const int rel = pos - real(step) * kTokens - 8 * half;   // tokens of the lane up to here are attended
+    if (masked) {
+      const int out = WINDOW ? rel - a.window : 0, in = WINDOW ? a.sinks - real(step) * kTokens - 8 * half : 0;   // but not up to there, unless before this
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[t][j] = 32 * t + 16 * (j >> 3) + (j & 7) <= rel ? x[t][j] : -INFINITY;
+        for (int j = 0; j < 16; ++j) {
+          const int i = 32 * t + 16 * (j >> 3) + (j & 7);
+          x[t][j] = i <= rel && (!WINDOW || i > out || i < in) ? x[t][j] : -INFINITY;
+        }
     }
     float top = x[0][0];
 #pragma unroll
@@ -188,14 +273,14 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
       }
       p[c] = pack8<BF16>(w);
     }
-    if constexpr (masked) {
+    if (known && masked) {
       // A row's weight of 0 must not meet a value that is no number: tokens behind the last one are cleared, and what else there is
       // of them is left out of the product; it is added after the last step.
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
-          u32x4 f = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32) & up_to_last(step * kTokens + 16 * c);
+          u32x4 f = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32) & up_to_last(real(step) * kTokens + 16 * c);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t odd = odd_halves<BF16>(f[j]);
@@ -208,23 +293,53 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
 #pragma unroll
       for (int at = 0; at < 4 * DT; at += kBatch) {
         if (at > 0) v_batch(at);
+        if (!known && masked) {   // the same as above
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) {
+            f[j] &= up_to_last(real(step) * kTokens + 16 * ((at + j) / DT));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t odd = odd_halves<BF16>(f[j][i]);
+              left_out |= odd;
+              f[j][i] &= ~odd;
+            }
+          }
+        }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) o[(at + j) % DT] = mfma32<BF16>(f[j], p[(at + j) / DT], o[(at + j) % DT]);
       }
     }
   };
 
+  auto turn = [&](int step) {
+    if constexpr (E4M3) {
+      lds_written();
+      if (step + TEAMS < steps) store(step + TEAMS);
+      if (step + 2 * TEAMS < steps) fetch(step + 2 * TEAMS);
+    } else {
+      lds_turn();
+      if (step + TEAMS < steps) load(step + TEAMS);
+    }
+  };
+  if constexpr (WINDOW) {
+    // Steps whose tokens all of the wave's rows attend, and others with a token that one of them does.
+    for (; step - team < steps; step += TEAMS) {
+      turn(step);
+      const int at = real(step) * kTokens, end = at + kTokens - 1;
+      if ((TEAMS > 1 && step >= steps) || at > wave_last || (end <= wave_first - a.window && at >= a.sinks)) continue;
+      work(step, !(end <= wave_first && (at > wave_last - a.window || end < a.sinks)));
+    }
+  } else {
   // First the steps whose tokens all of the wave's rows attend.
   const int whole = low < n && wave_first >= 0 ? (wave_first + 1) / kTokens : 0;
   for (; step < whole && step < steps; step += TEAMS) {
-    lds_turn();
-    if (step + TEAMS < steps) load(step + TEAMS);
+    turn(step);
     work(step, std::false_type());
   }
   for (; step - team < steps; step += TEAMS) {
-    lds_turn();
-    if (step + TEAMS < steps) load(step + TEAMS);
+    turn(step);
     if ((TEAMS == 1 || step < steps) && step * kTokens <= wave_last) work(step, std::true_type());
+  }
   }
 
   // A weight that rounds to 0 makes NaN of an infinite value, where the weight itself leaves infinity.  Where a sum is no number, though the
@@ -243,17 +358,26 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
     // 32 tokens at a time: what each row attends of them, with a weight (there) or without (none), times 1 for infinity, 64 for -infinity and
     // 4,096 for NaN: no more than 16 of each in a sum.  (4,096 tokens x 32 heads of 128 whose values are all NaN: 1.7 ms, 0.17 with none.)
     constexpr uint32_t kExp = BF16 ? 0x7f80 : 0x7c00, kOne = BF16 ? 0x3f80 : 0x3c00, k64 = BF16 ? 0x4280 : 0x5400, k4096 = BF16 ? 0x4580 : 0x6c00;
-    for (int at = (begin + team) * kTokens; at < steps * kTokens && at <= wave_last; at += at % kTokens ? 32 + (TEAMS - 1) * kTokens : 32) {
-      int64_t head[2];   // of the 16 tokens' page
+    for (int gone = (begin + team) * kTokens; gone < steps * kTokens; gone += gone % kTokens ? 32 + (TEAMS - 1) * kTokens : 32) {
+      const int at = real(gone / kTokens) * kTokens + gone % kTokens;
+      if (at > wave_last) break;
+      int64_t head[2], block[2];   // of the 16 tokens' page; their scales
       u32x4 keep[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int t = at + 16 * h, page = table[t >> shift < last_page ? t >> shift : last_page];
         head[h] = ((int64_t)page_inside(a.c, page) * a.c.kv_heads + kvh) * ((int64_t)D << shift);
+        block[h] = (((int64_t)page_inside(a.c, page) * a.c.kv_heads + kvh) << (shift - 4)) + ((t & mask) >> 4);
         keep[h] = up_to_last(t);
       }
       auto values = [&](int h, int i) {
-        return *reinterpret_cast<const u32x4*>(a.v_pages + head[h] + ((int64_t)(32 * i + col) << shift) + ((at + 16 * h) & mask) + 8 * half) & keep[h];
+        const int64_t from = head[h] + ((int64_t)(32 * i + col) << shift) + ((at + 16 * h) & mask) + 8 * half;
+        if constexpr (E4M3) {
+          const u32x2 u = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(a.v_pages) + from);
+          return values8<BF16>(u[0], u[1], a.v_scales[block[h]]) & keep[h];
+        } else {
+          return *reinterpret_cast<const u32x4*>(a.v_pages + from) & keep[h];
+        }
       };
       uint32_t odd = 0;
 #pragma unroll 1
@@ -265,15 +389,25 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
       f32x16 x;
 #pragma unroll
       for (int j = 0; j < 16; ++j) x[j] = 0.f;
-      const uint16_t* k = a.k_pages + (k_row < 16 ? head[0] : head[1]) + (((at + k_row) & mask) * D) + 8 * half;
+      const int64_t k_from = (k_row < 16 ? head[0] : head[1]) + (((at + k_row) & mask) * D) + 8 * half;
 #pragma unroll
-      for (int c = 0; c < KS; ++c) x = mfma32<BF16>(*reinterpret_cast<const u32x4*>(k + 16 * c), q[c], x);
+      for (int c = 0; c < KS; ++c) {
+        u32x4 f;
+        if constexpr (E4M3) {
+          const u32x2 u = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(a.k_pages) + k_from + 16 * c);
+          f = values8<BF16>(u[0], u[1], a.k_scales[k_row < 16 ? block[0] : block[1]]);
+        } else {
+          f = *reinterpret_cast<const u32x4*>(a.k_pages + k_from + 16 * c);
+        }
+        x = mfma32<BF16>(f, q[c], x);
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         u32x4 there = {0, 0, 0, 0}, none = {0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const bool mine = at + 16 * h + 8 * half + j <= pos, zero = x[8 * h + j] * a.scale_log2 == -INFINITY;
+          const int t = at + 16 * h + 8 * half + j;
+          const bool mine = t <= pos && (!WINDOW || t > pos - a.window || t < a.sinks), zero = x[8 * h + j] * a.scale_log2 == -INFINITY;
           there[j / 2] |= mine && !zero ? kOne << (j % 2 * 16) : 0u;
           none[j / 2] |= mine && zero ? kOne << (j % 2 * 16) : 0u;
         }
@@ -430,16 +564,25 @@ __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt_
   if (a.lse && half == 0 && valid) a.lse[(int64_t)(first + token) * a.heads + head] = any ? (m + __log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
-template <bool BF16, int D>
+// Instances by the plan: Kernels names the kernel of each.
+template <typename Kernels, bool BF16, int D>
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(a.a.heads / a.plan.heads * a.plan.slots), a.plan.parts);
   if constexpr (D <= 128)
     if (a.plan.teams == 2) {
-      prompt_kernel<BF16, D, 2><<<grid, 2 * 64 * kWaves, 0, s>>>(a);
+      Kernels::template kernel<BF16, D, 2><<<grid, 2 * 64 * kWaves, 0, s>>>(a);
       return hipGetLastError();
     }
-  prompt_kernel<BF16, D, 1><<<grid, 64 * kWaves, 0, s>>>(a);
+  Kernels::template kernel<BF16, D, 1><<<grid, 64 * kWaves, 0, s>>>(a);
   return hipGetLastError();
+}
+
+// Heads of 64, 96 and 128.
+template <typename Kernels, bool BF16>
+hipError_t launch_prompt_small(const PromptArgs& a, int head_dim, hipStream_t s) {
+  if (head_dim == 64) return launch_prompt<Kernels, BF16, 64>(a, s);
+  if (head_dim == 96) return launch_prompt<Kernels, BF16, 96>(a, s);
+  return launch_prompt<Kernels, BF16, 128>(a, s);
 }
 
 }  // namespace

@@ -129,11 +129,17 @@ __global__ __launch_bounds__(256) void copy_kernel(const CopyArgsOf<PAIRS> a) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (at + 4096 * i < a.page_bytes) __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4*>(to + at + 4096 * i));
+  if (piece == 0)   // pages in 8 bits
+    for (int i = threadIdx.x; i < a.scale_words; i += 256) {
+      uint32_t* scales = reinterpret_cast<uint32_t*>(base + a.scales_at);
+      scales[(int64_t)a.from_to[pair][1] * a.scale_words + i] = scales[(int64_t)a.from_to[pair][0] * a.scale_words + i];
+    }
 }
 
 }  // namespace
 
 hipError_t launch_append(const AppendArgs& a, int head_dim, hipStream_t s) {
+  if (a.k_scales) return launch_append8(a, head_dim, s);
   // Few new tokens for each sequence: most of a block of eight positions would be empty (64 sequences x 32 heads of 128, in the order of the
   // batched product: one new token each 7.6 us, 15.7 in blocks; two 11.9 and 16.2; four 19.5 and 17.5).  Few altogether: a block's
   // turn takes longer than they do (16 tokens of 8 sequences x 8 heads 5.0 and 8.5 us; 32 of one x 32 heads 5.8 and 6.0).

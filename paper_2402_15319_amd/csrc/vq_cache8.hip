@@ -1,0 +1,281 @@
+// New tokens' keys and values into pages in 8 bits.
+#include "vq_attn_device.h"
+
+namespace vq {
+namespace {
+
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;   // eight values wherever they lie
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+// Two values over a power of two, rounded to codes (nearest, ties to even) in the lower or upper half of a dword; what is no finite number becomes NaN.
+template <bool BF16, bool HIGH> __device__ __forceinline__ uint32_t codes2(uint32_t old, uint32_t pair, float scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  const s16x2 o = __builtin_bit_cast(s16x2, old);
+  if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(o, __builtin_bit_cast(bf16x2, pair), scale, HIGH));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(o, __builtin_bit_cast(f16x2, pair), scale, HIGH));
+}
+template <bool BF16> __device__ __forceinline__ u32x2 codes8(u32x4 v, float scale) {
+  return {codes2<BF16, true>(codes2<BF16, false>(0, v[0], scale), v[1], scale), codes2<BF16, true>(codes2<BF16, false>(0, v[2], scale), v[3], scale)};
+}
+
+// Magnitudes as 16-bit integers, which order as the numbers do.  1.875 * 2^15, or 2^127, is the largest whose nearest code at the largest scale is still
+// one of the type; 448 is 1.75 * 2^8.
+template <bool BF16> constexpr uint32_t kMost = BF16 ? 0x7f70 : 0x7b80;
+template <bool BF16> constexpr uint32_t kInfinite = BF16 ? 0x7f80 : 0x7c00;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+// The largest magnitude of the lane's values, as they count for a scale; those beyond the type's codes are brought into their range.
+template <bool BF16, int N> __device__ __forceinline__ uint32_t largest(u32x4 (&x)[N]) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = larger2(most, x[i][j] & 0x7fff7fffu);
+  most = (most & 0xffff) > most >> 16 ? most & 0xffff : most >> 16;
+  if (most <= kMost<BF16>) return most;
+  most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t at = j % 2 * 16, u = x[i][j / 2] >> at & 0x7fff, to = u >= kInfinite<BF16> ? 0x7fffu : u > kMost<BF16> ? kMost<BF16> : u;
+      x[i][j / 2] ^= (u ^ to) << at;
+      most = to < 0x7fff && to > most ? to : most;
+    }
+  return most;
+}
+
+// The smallest power of two, not below the type's least, that brings a magnitude to 448 or less.
+template <bool BF16> __device__ __forceinline__ float scale_for(uint32_t most) {
+  constexpr int kBits = BF16 ? 7 : 10, kBias = BF16 ? 127 : 15, kLeast = BF16 ? -117 : -15;
+  const int e = (int)((most + ((1 << kBits) - 1 - (3 << (kBits - 2)))) >> kBits) - kBias - 8;   // one more where the fraction is over .75
+  return __builtin_bit_cast(float, ((e > kLeast ? e : kLeast) + 127) << 23);
+}
+
+// Codes at a scale, rounded to a larger one.
+template <bool BF16> __device__ __forceinline__ u32x2 coarser(u32x2 codes, float from, float to) {
+  return codes8<BF16>(values8<BF16>(codes[0], codes[1], from), to);
+}
+
+// Eight by eight values, turned: in[i] holds (i, 0..7), out[j] (0..7, j).
+__device__ __forceinline__ void turn8(const u32x4 (&in)[8], u32x4 (&out)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[j][i] = __builtin_amdgcn_perm(in[2 * i + 1][j / 2], in[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+}
+
+// Where a token's head is, in heads of pages, or -1.
+__device__ __forceinline__ int64_t head_of(const CacheArgs& c, int s, int pos, int h) {
+  const int page = c.table[(int64_t)s * c.table_width + (pos >> c.page_shift)];
+  return (uint32_t)page < (uint32_t)c.n_pages ? (int64_t)page * c.kv_heads + h : -1;
+}
+
+constexpr int octets(int d) { return d == 64 ? 8 : d == 256 ? 32 : 16; }   // lanes for a head's dimensions, 8 each (of 16, those of 96 leave 4 idle)
+
+// One new token for each sequence: a lane takes eight dimensions of a head's key and value.  The block's earlier codes are
+// looked at only where its scale grows.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void append8_one_kernel(const AppendArgs a) {
+  constexpr int kLanes = octets(D);
+  const int t = blockIdx.x, i = blockIdx.y * 256 + threadIdx.x, h = i / kLanes, d = 8 * (i % kLanes);
+  const int pos = cached_tokens(a.c, t, kFarBeyond) - 1;
+  if (pos < 0 || pos >= a.c.max_len) return;
+  const bool there = h < a.c.kv_heads && d < D;
+  const int size = 1 << a.c.page_shift, slot = pos & (size - 1), kept = pos & (kBlock - 1);
+  const int64_t head = there ? head_of(a.c, t, pos, h) : -1;
+  const int64_t block = (head << (a.c.page_shift - 4)) + (slot >> 4);
+  u32x4 x[2][1] = {{{0, 0, 0, 0}}, {{0, 0, 0, 0}}};
+  float old[2] = {0.f, 0.f};
+  if (there) {
+    x[0][0] = gather8(a.k + t * a.ks.token + h * a.ks.head + d * a.ks.dim, a.ks.dim);
+    x[1][0] = gather8(a.v + t * a.vs.token + h * a.vs.head + d * a.vs.dim, a.vs.dim);
+  }
+  if (kept > 0 && head >= 0) {
+    old[0] = a.k_scales[block];
+    old[1] = a.v_scales[block];
+  }
+  uint32_t most[2] = {largest<BF16>(x[0]), largest<BF16>(x[1])};
+#pragma unroll
+  for (int w = 1; w < kLanes; w *= 2)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t other = __shfl_xor(most[j], w);
+      most[j] = other > most[j] ? other : most[j];
+    }
+  if (head < 0) return;
+  float scale[2];
+  u32x2 codes[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    scale[j] = fmaxf(scale_for<BF16>(most[j]), old[j]);
+    codes[j] = codes8<BF16>(x[j][0], scale[j]);
+  }
+  uint8_t* k = reinterpret_cast<uint8_t*>(a.k_pages) + (head << a.c.page_shift) * D + slot * D + d;
+  uint8_t* v = reinterpret_cast<uint8_t*>(a.v_pages) + (head << a.c.page_shift) * D + ((int64_t)d << a.c.page_shift) + slot;
+  *reinterpret_cast<u32x2*>(k) = codes[0];
+  if (kept > 0 && scale[0] > old[0])
+    for (int j = 1; j <= kept; ++j) {
+      u32x2* at = reinterpret_cast<u32x2*>(k - j * D);
+      *at = coarser<BF16>(*at, old[0], scale[0]);
+    }
+  if (kept > 0 && scale[1] > old[1]) {
+    for (int j = 0; j < 8; ++j) {   // a dimension's slots of the block at once
+      u32x4* at = reinterpret_cast<u32x4*>(v + j * size - kept);
+      const u32x4 was = *at;
+      u32x4 now;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const u32x2 u = coarser<BF16>(u32x2{was[2 * w], was[2 * w + 1]}, old[1], scale[1]);
+        now[2 * w] = u[0];
+        now[2 * w + 1] = u[1];
+      }
+      const uint32_t mine = codes[1][j / 4] >> (j % 4 * 8) & 0xff;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int n = kept - 4 * w;   // of this dword's slots, those before the new one
+        const uint32_t before = n >= 4 ? ~0u : n > 0 ? (1u << (8 * n)) - 1 : 0u, here = n >= 0 && n < 4 ? 0xffu << (8 * n) : 0u;
+        now[w] = (now[w] & before) | (mine * 0x01010101u & here) | (was[w] & ~before & ~here);
+      }
+      *at = now;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j * size] = (uint8_t)(codes[1][j / 4] >> (j % 4 * 8));
+  }
+  if (d == 0) {
+    a.k_scales[block] = scale[0];
+    a.v_scales[block] = scale[1];
+  }
+}
+
+// Any number of new tokens: a wave takes the keys, or the values, of one or more blocks of a head, a lane eight positions by eight dimensions in registers, and
+// the block's lanes exchange their largest magnitudes.  A workgroup is two waves for the keys of successive positions and two for the values.  Loads
+// are 16 bytes along whatever is contiguous in the source, stores 8 along what is in the page; in between the lane turns its block where those differ.
+template <int D> constexpr int kTile8 = 2 * 64 / octets(D) * 8;
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void append8_kernel(const AppendArgs a) {
+  constexpr int kLanes = octets(D), kOctets = 64 / kLanes;   // lanes for the dimensions, and for the positions
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool values = wave >= 2;
+  const int h = blockIdx.x % a.c.kv_heads;
+  const Tile tile = tile_of(a.c, blockIdx.x / a.c.kv_heads, kTile8<D>, 2, kFarBeyond);
+  const int s = tile.sequence, first = tile.first, last = tile.last;
+  const int behind = tile.cached - last, from = behind + first > 0 ? behind + first : 0;   // token t has position behind + t
+  const int stop = tile.cached < a.c.max_len ? tile.cached : a.c.max_len;
+  const int tile0 = (from / kTile8<D> + tile.number) * kTile8<D> + (wave & 1) * (kOctets * 8);
+  if (last <= first || from >= stop || tile0 >= stop || tile0 + kOctets * 8 <= (from & -kBlock)) return;   // the wave has no block with a new token
+  // lanes: positions first where the source runs along them, dimensions first where it runs along those
+  const Strides st = values ? a.vs : a.ks;
+  const bool along_tokens = st.token == 1 && st.dim != 1;
+  const int x = along_tokens ? lane % kOctets : lane / kLanes, y = along_tokens ? lane / kOctets : lane % kLanes;
+  const int pos = tile0 + 8 * x, block0 = pos & -kBlock;
+  // Its dimensions: 8 y .. + 7, or, where nothing is turned, every kLanes-th from y, so that the lanes of an instruction have successive ones.
+  const bool spread = D % 64 == 0 && values && along_tokens;
+  const int d = spread ? y : 8 * y, d_step = spread ? kLanes : 1;
+  const int64_t dim = st.dim * d_step;
+  // Of its positions lo .. hi - 1 are new and have a place, and those before `kept` hold earlier tokens of the block.
+  const bool mine = d < D && block0 < stop && block0 + kBlock > from;
+  const int lo = from - pos > 0 ? from - pos : 0, hi = mine ? (stop - pos < 8 ? stop - pos : 8) : 0;
+  const int kept = mine ? (lo < 8 ? lo : 8) : 0;
+  const int64_t head = mine ? head_of(a.c, s, pos, h) : -1;
+  const int size = 1 << a.c.page_shift, slot = pos & (size - 1);
+  float* scales = (values ? a.v_scales : a.k_scales) + (head << (a.c.page_shift - 4)) + (slot >> 4);
+  const float old = mine && head >= 0 && from > block0 ? *scales : 0.f;
+  const bool whole = lo == 0 && hi == 8;
+  u32x4 in[8], turned[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) in[i] = {0, 0, 0, 0};
+  bool by_token = true;   // in[i] is position i's dimensions; otherwise dimension i's positions
+  if (lo < hi) {
+    const uint16_t* src = (values ? a.v : a.k) + (int64_t)(pos - behind) * st.token + h * st.head + d * st.dim;
+    if (st.dim == 1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) in[i] = *reinterpret_cast<const u32x4_any*>(src + (i < lo ? lo : i < hi ? i : hi - 1) * st.token);
+    } else if (st.token == 1 && whole) {
+      by_token = false;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) in[i] = *reinterpret_cast<const u32x4_any*>(src + i * dim);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) in[i] = gather8(src + (i < lo ? lo : i < hi ? i : hi - 1) * st.token, dim);
+    }
+  }
+  uint32_t most = largest<BF16>(in);   // (positions that are not new repeat one that is)
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) {
+    if (along_tokens ? w > 1 && w < kOctets : w > kLanes) continue;   // other blocks' lanes
+    const uint32_t other = __shfl_xor(most, w);
+    most = other > most ? other : most;
+  }
+  if (head < 0) return;
+  const float scale = fmaxf(scale_for<BF16>(most), old);
+  const bool grows = kept > 0 && scale > old;
+  if (by_token == values) {
+    turn8(in, turned);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) in[i] = turned[i];
+  }
+  if (!values) {
+    uint8_t* to = reinterpret_cast<uint8_t*>(a.k_pages) + (head << a.c.page_shift) * D + slot * D + d;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      u32x2* at = reinterpret_cast<u32x2*>(to + i * D);
+      if (i >= lo && i < hi) *at = codes8<BF16>(in[i], scale);
+      else if (grows && i < kept) *at = coarser<BF16>(*at, old, scale);
+    }
+  } else {
+    uint8_t* to = reinterpret_cast<uint8_t*>(a.v_pages) + (head << a.c.page_shift) * D + ((int64_t)d << a.c.page_shift) + slot;
+    const int step = d_step * size;
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x2*>(to + i * step) = codes8<BF16>(in[i], scale);
+    } else if (lo < hi || grows) {   // other tokens' slots stay as they are
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u32x2* at = reinterpret_cast<u32x2*>(to + i * step);
+        const u32x2 was = *at, fresh = codes8<BF16>(in[i], scale), moved = grows ? coarser<BF16>(was, old, scale) : was;
+        u32x2 now;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          uint32_t keep = 0, put = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            keep |= 4 * w + j < kept ? 0xffu << (8 * j) : 0u;
+            put |= 4 * w + j >= lo && 4 * w + j < hi ? 0xffu << (8 * j) : 0u;
+          }
+          now[w] = (moved[w] & keep) | (fresh[w] & put) | (was[w] & ~keep & ~put);
+        }
+        *at = now;
+      }
+    }
+  }
+  if (d == 0 && pos == block0) *scales = scale;
+}
+
+template <bool BF16, int D>
+hipError_t launch_dim(const AppendArgs& a, hipStream_t s) {
+  if (!a.c.q_start) append8_one_kernel<BF16, D><<<dim3(a.c.n_tokens, (a.c.kv_heads * octets(D) + 255) / 256), 256, 0, s>>>(a);
+  else append8_kernel<BF16, D><<<(unsigned)((a.c.n_tokens / kTile8<D> + 2 * (int64_t)a.c.n_seqs) * a.c.kv_heads), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t launch_type(const AppendArgs& a, int head_dim, hipStream_t s) {
+  if (head_dim == 64) return launch_dim<BF16, 64>(a, s);
+  if (head_dim == 96) return launch_dim<BF16, 96>(a, s);
+  if (head_dim == 128) return launch_dim<BF16, 128>(a, s);
+  return launch_dim<BF16, 256>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_append8(const AppendArgs& a, int head_dim, hipStream_t s) {
+  return a.bf16 ? launch_type<true>(a, head_dim, s) : launch_type<false>(a, head_dim, s);
+}
+
+}  // namespace vq
