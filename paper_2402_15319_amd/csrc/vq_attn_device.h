@@ -95,6 +95,15 @@ template <bool BF16> __device__ __forceinline__ u32x4 pack8(f32x8 p) {
   else return __builtin_bit_cast(u32x4, __builtin_convertvector(p, f16x8));
 }
 
+// The larger, and the smaller, of each two halves, as integers: of magnitudes, the larger or smaller number.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+__device__ __forceinline__ uint32_t smaller2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 // Eight codes (e4m3, two dwords) as values of the cache's type: exactly, for a block's scale is a power of two that leaves every code a
 // number of the type.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));

@@ -24,7 +24,8 @@ template <int D> __device__ __forceinline__ int k_turn(int r) {
 // K and V^T of a step come into LDS past the registers, each wave 16 tokens of both (one page), while the step before is
 // worked on.  With two teams of such waves (see the plan) each takes every second step, and the second's sums go to the first in the end.
 // E4M3: pages in 8 bits.  A wave's 16 tokens are one block; their codes come into registers while the step before the one before is worked on, and go
-// to LDS as values of the type (exactly), each once for the workgroup, so that the products are those of 16 bits.
+// to LDS as values of the type (exactly), each once for the workgroup, so that the products are those of 16 bits.  Tokens that no row sees and
+// values that are no numbers stay behind on the way, so that no step looks for them again.
 // WINDOW: a.window and a.sinks.  What no row of the tile sees between the sinks and the window, in whole steps, is passed over: `step` counts the
 // steps that are gone through, real(step) is the place of one in the sequence.
 template <bool BF16, int D, int TEAMS, bool E4M3, bool WINDOW>
@@ -33,6 +34,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   constexpr int KS = D / 16, DT = D / 32, kLoads = D / 32;     // loads of a wave for its 16 tokens' K, and for their V
   constexpr int kHalf = kTokens * D * 2, kStep = 2 * kHalf;    // bytes of K, or V, of a step
   __shared__ __attribute__((aligned(1024))) char lds[TEAMS * 2 * kStep];
+  __shared__ uint32_t odd_codes[kWaves * TEAMS];   // E4M3: values that are no numbers, by the waves that brought them
   const int tid = threadIdx.x, number = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = number % kWaves, team = number / kWaves;
   // The heads are neighbours, and so are on the 8 XCDs in turn: those of an XCD keep to their keys and values.  Of the tiles the last come
@@ -119,16 +121,16 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   };
   // The same in 8 bits, in two halves.  16 codes of a token's dimensions, or of a dimension's tokens, to a load; of heads of 96 the last 32 dimensions
   // are 8 to a load.
+  const int this_lane = lane;
   constexpr int kCodes = D / 64, kFrags = (D + 63) / 64;
   u32x4 k_codes[E4M3 ? kFrags : 1], v_codes[E4M3 ? kFrags : 1];
   float k_scale = 1.f, v_scale = 1.f;
-  auto here = [&]() {   // the lane, from which the places below are made again in every step: kept, they would take registers of the products
-    int x = lane;
+  auto apart = [](int x) {   // the same number, but nothing is made of it beforehand or for another place: that would take registers of the products
     asm volatile("" : "+v"(x));
     return x;
   };
   auto fetch = [&](int step) {
-    const int lane = here();
+    const int lane = apart(this_lane);
     const int page = page_of(step);
     const int in = (real(step) * kTokens + 16 * wave) & mask;
     const int64_t head = (int64_t)page * a.c.kv_heads + kvh;
@@ -150,7 +152,39 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     }
   };
   auto store = [&](int step) {
-    const int lane = here();
+    const int lane = apart(this_lane);
+    const int first = real(step) * kTokens;
+    if (first + kTokens > len || (first < first_seen && first + kTokens > a.sinks)) {
+      const int at = apart(first + 16 * wave);
+      auto seen = [&](int t) { return t < len && (t < a.sinks || t >= first_seen); };
+      u32x4 keep = {0, 0, 0, 0};
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        keep[i / 4] |= seen(at + i) ? 0xffu << (i % 4 * 8) : 0u;
+        any |= seen(at + i);
+      }
+#pragma unroll
+      for (int j = 0; j < kCodes; ++j) v_codes[j] &= keep;
+      if constexpr (E4M3 && kFrags > kCodes) {
+        v_codes[kCodes][0] &= lane & 1 ? keep[2] : keep[0];
+        v_codes[kCodes][1] &= lane & 1 ? keep[3] : keep[1];
+      }
+      v_scale = any ? v_scale : 1.f;   // a block without a token has a scale of any kind
+    }
+    auto odd = [](uint32_t c) { return ((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };
+    uint32_t some = 0;
+#pragma unroll
+    for (int j = 0; j < (E4M3 ? kFrags : 1); ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) some |= odd(v_codes[j][e]);
+    if (__builtin_expect(__any(some), 0)) {
+#pragma unroll
+      for (int j = 0; j < (E4M3 ? kFrags : 1); ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v_codes[j][e] &= ~((odd(v_codes[j][e]) >> 7) * 0xffu);
+      odd_codes[number] = 1;
+    }
     char* to = lds + (2 * team + ((step / TEAMS) & 1)) * kStep + wave * (kHalf / kWaves);
     auto k_piece = [&](int at, u32x4 v) {   // of 8 dimensions: the at-th of the wave's tokens, one token after another
       const int r = at / (D / 8), p = at % (D / 8);
@@ -173,6 +207,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
 
   int step = begin + team;
   if constexpr (E4M3) {
+    odd_codes[number] = 0;
     if (step < steps) {
       fetch(step);
       store(step);
@@ -238,13 +273,14 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     __builtin_amdgcn_s_setprio(0);
     const int rel = pos - real(step) * kTokens - 8 * half;   // tokens of the lane up to here are attended
     if (masked) {
-      const int out = WINDOW ? rel - a.window : 0, in = WINDOW ? a.sinks - real(step) * kTokens - 8 * half : 0;   // but not up to there, unless before this
+      const uint32_t wide = WINDOW ? (uint32_t)a.window : 0;
+      const int sinks = WINDOW ? a.sinks - real(step) * kTokens - 8 * half : 0, in = sinks < rel + 1 ? sinks : rel + 1;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const int i = 32 * t + 16 * (j >> 3) + (j & 7);
-          x[t][j] = i <= rel && (!WINDOW || i > out || i < in) ? x[t][j] : -INFINITY;
+          x[t][j] = (WINDOW ? (uint32_t)(rel - i) < wide || i < in : i <= rel) ? x[t][j] : -INFINITY;
         }
     }
     float top = x[0][0];
@@ -293,17 +329,26 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
 #pragma unroll
       for (int at = 0; at < 4 * DT; at += kBatch) {
         if (at > 0) v_batch(at);
-        if (!known && masked) {   // the same as above
+        if (!E4M3 && !known && masked) {
+          // To the same end every magnitude is brought to the largest finite one, and whether that changes a token that some row may see is
+          // looked at on the way: half the instructions.  (What such a value then adds to a row that sees it, infinity or NaN makes away with.)
+          const int first = real(step) * kTokens;
+          const bool clear = first + kTokens > len || (first < first_seen && first + kTokens > a.sinks);
+          uint32_t size = 0;   // the largest magnitudes of both halves, as integers
 #pragma unroll
-          for (int j = 0; j < kBatch; ++j) {
-            f[j] &= up_to_last(real(step) * kTokens + 16 * ((at + j) / DT));
+          for (int c = 0; c < kBatch / DT; ++c) {
+            u32x4 keep = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
+            if (clear) keep &= up_to_last(apart(first + 16 * (at / DT + c)));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t odd = odd_halves<BF16>(f[j][i]);
-              left_out |= odd;
-              f[j][i] &= ~odd;
-            }
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t v = f[c * DT + i][e];
+                size = larger2(size, v & keep[e]);
+                f[c * DT + i][e] = (v & 0x80008000u) | smaller2(v & 0x7fff7fffu, BF16 ? 0x7f7f7f7fu : 0x7bff7bffu);
+              }
           }
+          left_out |= odd_halves<BF16>(size);
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) o[(at + j) % DT] = mfma32<BF16>(f[j], p[(at + j) / DT], o[(at + j) % DT]);
@@ -350,6 +395,10 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) largest = __builtin_elementwise_maximum(largest, o[i][j]);   // NaN where one of them is
+  if constexpr (E4M3) {
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) left_out |= odd_codes[kWaves * team + i];
+  }
   if (__builtin_expect(__any(left_out != 0 || (__builtin_isunordered(largest, largest) && !__builtin_isunordered(l, l))), 0)) {
 #pragma unroll
     for (int i = 0; i < DT; ++i)

@@ -23,10 +23,6 @@ template <bool BF16> __device__ __forceinline__ u32x2 codes8(u32x4 v, float scal
 // one of the type; 448 is 1.75 * 2^8.
 template <bool BF16> constexpr uint32_t kMost = BF16 ? 0x7f70 : 0x7b80;
 template <bool BF16> constexpr uint32_t kInfinite = BF16 ? 0x7f80 : 0x7c00;
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
 
 // The largest magnitude of the lane's values, as they count for a scale; those beyond the type's codes are brought into their range.
 template <bool BF16, int N> __device__ __forceinline__ uint32_t largest(u32x4 (&x)[N]) {
