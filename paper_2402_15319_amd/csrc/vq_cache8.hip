@@ -73,115 +73,119 @@ __device__ __forceinline__ int64_t head_of(const CacheArgs& c, int s, int pos, i
 
 constexpr int octets(int d) { return d == 64 ? 8 : d == 256 ? 32 : 16; }   // lanes for a head's dimensions, 8 each (of 16, those of 96 leave 4 idle)
 
-// One new token for each sequence: a lane takes eight dimensions of a head's key and value.  The block's earlier codes are
-// looked at only where its scale grows.
+// Few new tokens for each sequence: the threads of a token take eight dimensions of a head's key and value each.  They look at the block's other new tokens,
+// if there are any, for its scale; those of the first one also see to the earlier tokens' codes, where the scale grows, and to the scale.  (Another token's
+// threads may find the new scale in place of the old one: theirs is the same from either.)
 template <bool BF16, int D>
-__global__ __launch_bounds__(256) void append8_one_kernel(const AppendArgs a) {
+__global__ __launch_bounds__(256) void append8_few_kernel(const AppendArgs a) {
   constexpr int kLanes = octets(D);
   const int t = blockIdx.x, i = blockIdx.y * 256 + threadIdx.x, h = i / kLanes, d = 8 * (i % kLanes);
-  const int pos = cached_tokens(a.c, t, kFarBeyond) - 1;
-  if (pos < 0 || pos >= a.c.max_len) return;
+  const Tile tile = a.c.q_start ? tile_of(a.c, t, 1, 0, kFarBeyond) : Tile{t, 0, t, t + 1, cached_tokens(a.c, t, kFarBeyond)};
+  const int s = tile.sequence, pos = tile.cached - tile.last + t;
+  if (t < tile.first || t >= tile.last || pos < 0 || pos >= a.c.max_len) return;
+  const int size = 1 << a.c.page_shift, slot = pos & (size - 1), in = pos & (kBlock - 1);
+  // the block's new tokens, and how many earlier ones lie before them
+  const int first = t - in > tile.first ? t - in : tile.first, last = t - in + kBlock < tile.last ? t - in + kBlock : tile.last;
+  const int beyond = t + (a.c.max_len - pos), stop = last < beyond ? last : beyond, kept = in - (t - first);
   const bool there = h < a.c.kv_heads && d < D;
-  const int size = 1 << a.c.page_shift, slot = pos & (size - 1), kept = pos & (kBlock - 1);
-  const int64_t head = there ? head_of(a.c, t, pos, h) : -1;
-  const int64_t block = (head << (a.c.page_shift - 4)) + (slot >> 4);
   u32x4 x[2][1] = {{{0, 0, 0, 0}}, {{0, 0, 0, 0}}};
+  uint32_t most[2] = {0, 0};
+  const uint16_t* k_from = a.k + h * a.ks.head + d * a.ks.dim;
+  const uint16_t* v_from = a.v + h * a.vs.head + d * a.vs.dim;
+  auto look = [&](int j) {
+    if (there) {
+      x[0][0] = gather8(k_from + j * a.ks.token, a.ks.dim);
+      x[1][0] = gather8(v_from + j * a.vs.token, a.vs.dim);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t now = largest<BF16>(x[e]);
+      most[e] = now > most[e] ? now : most[e];
+    }
+  };
+#pragma unroll 1
+  for (int j = first; j < stop; ++j)
+    if (j != t) look(j);
+  look(t);   // the last one: its values stay
+  const int64_t head = there ? head_of(a.c, s, pos, h) : -1;
+  const int64_t block = (head << (a.c.page_shift - 4)) + (slot >> 4);
   float old[2] = {0.f, 0.f};
-  if (there) {
-    x[0][0] = gather8(a.k + t * a.ks.token + h * a.ks.head + d * a.ks.dim, a.ks.dim);
-    x[1][0] = gather8(a.v + t * a.vs.token + h * a.vs.head + d * a.vs.dim, a.vs.dim);
-  }
   if (kept > 0 && head >= 0) {
     old[0] = a.k_scales[block];
     old[1] = a.v_scales[block];
   }
-  uint32_t most[2] = {largest<BF16>(x[0]), largest<BF16>(x[1])};
 #pragma unroll
   for (int w = 1; w < kLanes; w *= 2)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t other = __shfl_xor(most[j], w);
-      most[j] = other > most[j] ? other : most[j];
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t other = __shfl_xor(most[e], w);
+      most[e] = other > most[e] ? other : most[e];
     }
   if (head < 0) return;
-  float scale[2];
-  u32x2 codes[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    scale[j] = fmaxf(scale_for<BF16>(most[j]), old[j]);
-    codes[j] = codes8<BF16>(x[j][0], scale[j]);
-  }
+  const float scale[2] = {fmaxf(scale_for<BF16>(most[0]), old[0]), fmaxf(scale_for<BF16>(most[1]), old[1])};
   uint8_t* k = reinterpret_cast<uint8_t*>(a.k_pages) + (head << a.c.page_shift) * D + slot * D + d;
   uint8_t* v = reinterpret_cast<uint8_t*>(a.v_pages) + (head << a.c.page_shift) * D + ((int64_t)d << a.c.page_shift) + slot;
-  *reinterpret_cast<u32x2*>(k) = codes[0];
+  *reinterpret_cast<u32x2*>(k) = codes8<BF16>(x[0][0], scale[0]);
+  const u32x2 codes = codes8<BF16>(x[1][0], scale[1]);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e * size] = (uint8_t)(codes[e / 4] >> (e % 4 * 8));
+  if (t != first) return;
   if (kept > 0 && scale[0] > old[0])
+#pragma unroll 1
     for (int j = 1; j <= kept; ++j) {
       u32x2* at = reinterpret_cast<u32x2*>(k - j * D);
       *at = coarser<BF16>(*at, old[0], scale[0]);
     }
-  if (kept > 0 && scale[1] > old[1]) {
-    for (int j = 0; j < 8; ++j) {   // a dimension's slots of the block at once
-      u32x4* at = reinterpret_cast<u32x4*>(v + j * size - kept);
-      const u32x4 was = *at;
-      u32x4 now;
+  if (kept > 0 && scale[1] > old[1])
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {   // a dimension's slots of the block are read at once; other tokens may be writing theirs
+      uint8_t* at = v + e * size - kept;
+      const u32x4 was = *reinterpret_cast<const u32x4*>(at);
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        const u32x2 u = coarser<BF16>(u32x2{was[2 * w], was[2 * w + 1]}, old[1], scale[1]);
-        now[2 * w] = u[0];
-        now[2 * w + 1] = u[1];
-      }
-      const uint32_t mine = codes[1][j / 4] >> (j % 4 * 8) & 0xff;
+        const u32x2 now = coarser<BF16>(u32x2{was[2 * w], was[2 * w + 1]}, old[1], scale[1]);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int n = kept - 4 * w;   // of this dword's slots, those before the new one
-        const uint32_t before = n >= 4 ? ~0u : n > 0 ? (1u << (8 * n)) - 1 : 0u, here = n >= 0 && n < 4 ? 0xffu << (8 * n) : 0u;
-        now[w] = (now[w] & before) | (mine * 0x01010101u & here) | (was[w] & ~before & ~here);
+        for (int j = 0; j < 8; ++j)
+          if (8 * w + j < kept) at[8 * w + j] = (uint8_t)(now[j / 4] >> (j % 4 * 8));
       }
-      *at = now;
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j * size] = (uint8_t)(codes[1][j / 4] >> (j % 4 * 8));
-  }
   if (d == 0) {
     a.k_scales[block] = scale[0];
     a.v_scales[block] = scale[1];
   }
 }
 
-// Any number of new tokens: a wave takes the keys, or the values, of one or more blocks of a head, a lane eight positions by eight dimensions in registers, and
-// the block's lanes exchange their largest magnitudes.  A workgroup is two waves for the keys of successive positions and two for the values.  Loads
-// are 16 bytes along whatever is contiguous in the source, stores 8 along what is in the page; in between the lane turns its block where those differ.
-template <int D> constexpr int kTile8 = 2 * 64 / octets(D) * 8;
+// Any number of new tokens: a workgroup takes 64 positions of a sequence and a head, half of its waves the keys and half the values, a wave 64 of the
+// dimensions, a lane eight positions by eight dimensions in registers.  The lanes and waves that have a block exchange their largest magnitudes.  Loads
+// are 16 bytes along whatever is contiguous in the source, 128 in a row of lanes, stores 8 along what is in the page; in between the lane turns its block where
+// those differ.
+constexpr int kTile8 = 64;
 template <bool BF16, int D>
-__global__ __launch_bounds__(256) void append8_kernel(const AppendArgs a) {
-  constexpr int kLanes = octets(D), kOctets = 64 / kLanes;   // lanes for the dimensions, and for the positions
+__global__ __launch_bounds__(128 * ((D + 63) / 64)) void append8_kernel(const AppendArgs a) {
+  constexpr int kParts = (D + 63) / 64;   // waves for the dimensions
+  __shared__ uint32_t of_blocks[2 * kParts][kTile8 / kBlock];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool values = wave >= 2;
+  const bool values = wave >= kParts;
   const int h = blockIdx.x % a.c.kv_heads;
-  const Tile tile = tile_of(a.c, blockIdx.x / a.c.kv_heads, kTile8<D>, 2, kFarBeyond);
+  const Tile tile = tile_of(a.c, blockIdx.x / a.c.kv_heads, kTile8, 2, kFarBeyond);
   const int s = tile.sequence, first = tile.first, last = tile.last;
   const int behind = tile.cached - last, from = behind + first > 0 ? behind + first : 0;   // token t has position behind + t
   const int stop = tile.cached < a.c.max_len ? tile.cached : a.c.max_len;
-  const int tile0 = (from / kTile8<D> + tile.number) * kTile8<D> + (wave & 1) * (kOctets * 8);
-  if (last <= first || from >= stop || tile0 >= stop || tile0 + kOctets * 8 <= (from & -kBlock)) return;   // the wave has no block with a new token
+  const int tile0 = (from / kTile8 + tile.number) * kTile8;
+  if (last <= first || from >= stop || tile0 >= stop) return;        // no new token: for the whole workgroup
   // lanes: positions first where the source runs along them, dimensions first where it runs along those
   const Strides st = values ? a.vs : a.ks;
   const bool along_tokens = st.token == 1 && st.dim != 1;
-  const int x = along_tokens ? lane % kOctets : lane / kLanes, y = along_tokens ? lane / kOctets : lane % kLanes;
+  const int x = along_tokens ? lane & 7 : lane >> 3, y = along_tokens ? lane >> 3 : lane & 7;
   const int pos = tile0 + 8 * x, block0 = pos & -kBlock;
-  // Its dimensions: 8 y .. + 7, or, where nothing is turned, every kLanes-th from y, so that the lanes of an instruction have successive ones.
+  // Its dimensions: 8 y .. + 7, or, where nothing is turned, every eighth from y, so that the lanes of an instruction have successive ones.
   const bool spread = D % 64 == 0 && values && along_tokens;
-  const int d = spread ? y : 8 * y, d_step = spread ? kLanes : 1;
+  const int d = 64 * (wave % kParts) + (spread ? y : 8 * y), d_step = spread ? 8 : 1;
   const int64_t dim = st.dim * d_step;
   // Of its positions lo .. hi - 1 are new and have a place, and those before `kept` hold earlier tokens of the block.
   const bool mine = d < D && block0 < stop && block0 + kBlock > from;
   const int lo = from - pos > 0 ? from - pos : 0, hi = mine ? (stop - pos < 8 ? stop - pos : 8) : 0;
   const int kept = mine ? (lo < 8 ? lo : 8) : 0;
-  const int64_t head = mine ? head_of(a.c, s, pos, h) : -1;
-  const int size = 1 << a.c.page_shift, slot = pos & (size - 1);
-  float* scales = (values ? a.v_scales : a.k_scales) + (head << (a.c.page_shift - 4)) + (slot >> 4);
-  const float old = mine && head >= 0 && from > block0 ? *scales : 0.f;
   const bool whole = lo == 0 && hi == 8;
   u32x4 in[8], turned[8];
 #pragma unroll
@@ -189,7 +193,10 @@ __global__ __launch_bounds__(256) void append8_kernel(const AppendArgs a) {
   bool by_token = true;   // in[i] is position i's dimensions; otherwise dimension i's positions
   if (lo < hi) {
     const uint16_t* src = (values ? a.v : a.k) + (int64_t)(pos - behind) * st.token + h * st.head + d * st.dim;
-    if (st.dim == 1) {
+    if (st.dim == 1 && whole) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) in[i] = *reinterpret_cast<const u32x4_any*>(src + i * st.token);
+    } else if (st.dim == 1) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) in[i] = *reinterpret_cast<const u32x4_any*>(src + (i < lo ? lo : i < hi ? i : hi - 1) * st.token);
     } else if (st.token == 1 && whole) {
@@ -201,12 +208,34 @@ __global__ __launch_bounds__(256) void append8_kernel(const AppendArgs a) {
       for (int i = 0; i < 8; ++i) in[i] = gather8(src + (i < lo ? lo : i < hi ? i : hi - 1) * st.token, dim);
     }
   }
+  // (the source does not wait for the table)
+  const int64_t head = mine ? head_of(a.c, s, pos, h) : -1;
+  const int size = 1 << a.c.page_shift, slot = pos & (size - 1);
+  float* scales = (values ? a.v_scales : a.k_scales) + (head << (a.c.page_shift - 4)) + (slot >> 4);
+  const float old = head >= 0 && from > block0 ? *scales : 0.f;
   uint32_t most = largest<BF16>(in);   // (positions that are not new repeat one that is)
-#pragma unroll
-  for (int w = 1; w < 64; w *= 2) {
-    if (along_tokens ? w > 1 && w < kOctets : w > kLanes) continue;   // other blocks' lanes
+  auto exchange = [&](int w) {
     const uint32_t other = __shfl_xor(most, w);
     most = other > most ? other : most;
+  };
+  // the lanes with the block's other positions and the wave's other dimensions, then the waves with other dimensions
+  exchange(1);
+  exchange(8);
+  if (along_tokens) {
+    exchange(16);
+    exchange(32);
+  } else {
+    exchange(2);
+    exchange(4);
+  }
+  if constexpr (kParts > 1) {
+    if (y == 0) of_blocks[wave][x >> 1] = most;   // (two lanes, the same number)
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      const uint32_t other = of_blocks[(values ? kParts : 0) + i][x >> 1];
+      most = other > most ? other : most;
+    }
   }
   if (head < 0) return;
   const float scale = fmaxf(scale_for<BF16>(most), old);
@@ -218,11 +247,16 @@ __global__ __launch_bounds__(256) void append8_kernel(const AppendArgs a) {
   }
   if (!values) {
     uint8_t* to = reinterpret_cast<uint8_t*>(a.k_pages) + (head << a.c.page_shift) * D + slot * D + d;
+    if (whole) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      u32x2* at = reinterpret_cast<u32x2*>(to + i * D);
-      if (i >= lo && i < hi) *at = codes8<BF16>(in[i], scale);
-      else if (grows && i < kept) *at = coarser<BF16>(*at, old, scale);
+      for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x2*>(to + i * D) = codes8<BF16>(in[i], scale);
+    } else if (lo < hi || grows) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u32x2* at = reinterpret_cast<u32x2*>(to + i * D);
+        if (i >= lo && i < hi) *at = codes8<BF16>(in[i], scale);
+        else if (grows && i < kept) *at = coarser<BF16>(*at, old, scale);
+      }
     }
   } else {
     uint8_t* to = reinterpret_cast<uint8_t*>(a.v_pages) + (head << a.c.page_shift) * D + ((int64_t)d << a.c.page_shift) + slot;
@@ -255,8 +289,11 @@ __global__ __launch_bounds__(256) void append8_kernel(const AppendArgs a) {
 
 template <bool BF16, int D>
 hipError_t launch_dim(const AppendArgs& a, hipStream_t s) {
-  if (!a.c.q_start) append8_one_kernel<BF16, D><<<dim3(a.c.n_tokens, (a.c.kv_heads * octets(D) + 255) / 256), 256, 0, s>>>(a);
-  else append8_kernel<BF16, D><<<(unsigned)((a.c.n_tokens / kTile8<D> + 2 * (int64_t)a.c.n_seqs) * a.c.kv_heads), 256, 0, s>>>(a);
+  // Few new tokens for each sequence: most of a tile would be empty.
+  if (!a.c.q_start || a.c.n_tokens <= 2 * (int64_t)a.c.n_seqs)
+    append8_few_kernel<BF16, D><<<dim3(a.c.n_tokens, (a.c.kv_heads * octets(D) + 255) / 256), 256, 0, s>>>(a);
+  else
+    append8_kernel<BF16, D><<<(unsigned)((a.c.n_tokens / kTile8 + 2 * (int64_t)a.c.n_seqs) * a.c.kv_heads), 128 * ((D + 63) / 64), 0, s>>>(a);
   return hipGetLastError();
 }
 

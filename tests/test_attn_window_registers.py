@@ -21,7 +21,7 @@ def test_every_instance_is_one_that_a_plan_names(resources):  # noqa: F811
     assert set(_decode(resources, "decode8_kernel")) == {(b, d, lines, w, t) for b in (0, 1) for lines in (0, 1) for d, w, t in shapes}
     for kernel in ("prompt_window_kernel", "prompt8_kernel"):
         assert sum(kernel in n for n in resources) == 2 * 7
-    assert sum("append8_one_kernel" in n for n in resources) == sum("append8_kernel" in n for n in resources) == 8
+    assert sum("append8_few_kernel" in n for n in resources) == sum("append8_kernel" in n for n in resources) == 8
 
 
 def test_scratch(resources):  # noqa: F811
