@@ -110,6 +110,7 @@ constexpr int64_t kEnoughUnits = 256;
 constexpr int64_t kTogetherUnits = 16;
 constexpr int kLongPart = 4096, kShortPart = 1024;
 constexpr int kShortValues = 32768;       // of a sequence's keys: no parts up to here
+int short_values(const vq_attn_desc& d) { return eight_bits(d) ? 2 * kShortValues : kShortValues; }   // as many bytes
 int most_together(const vq_attn_desc& d) { return eight_bits(d) && d.head_dim > kThreeDim8 ? 2 : 3; }
 
 // What of a sequence of max_len tokens a new one goes through: the sinks and the window, to whole steps of a wave.
@@ -126,7 +127,29 @@ int64_t prompt_seen(int64_t max_len, const vq_attn_window* w) {
   return seen < max_len ? seen : max_len;
 }
 
-DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
+// Parts of sequences that are as good as alike, as most are where a window cuts them to half of the longest or less: `steps` steps each, `units` workgroups to a part.  A
+// compute unit draws at most about 1/160 of what the memory gives, so that time goes by whole workgroups to a compute unit: those of the last round, fewer than
+// 256, have it faster or for themselves.  In steps of such a workgroup, (per + 0.3) (1.55 f + r) with f whole rounds and r = max(1, rest / 160) for a rest, and
+// 0.5 + 0.15 parts for a join of heads of 128.  Fitted to windows of 1,000 and 4,000 x 1 to 80 sequences x 8 heads, in 8 bits and 16; of the parts measured (1 to
+// 16) it takes the best or one within 4 %, where lengths alone (kLongPart, kShortPart) were up to 30 % off: 20 sequences, window of 1,000, 8 bits: 11.5 us
+// in one part, 15.0 in two; 10 sequences, 4,000, 16 bits: 28.1 in three, 34.6 in four.
+constexpr int64_t kMostAlike = 1280;      // workgroups that parts make of them at most
+int64_t parts_alike(const vq_attn_desc& d, int64_t units, int64_t steps) {
+  int64_t best = 1;
+  double least = 0;
+  for (int64_t p = 1; p <= steps && p <= kMostParts && (p == 1 || units * p <= kMostAlike); ++p) {
+    const int64_t per = (steps + p - 1) / p, n = units * ((steps + per - 1) / per), f = n / kEnoughUnits, rest = n % kEnoughUnits;
+    const double r = rest == 0 ? 0. : rest > 160 ? rest / 160. : 1., join = p > 1 ? (0.5 + 0.15 * p) * 128 / d.head_dim : 0.;
+    const double time = (per + 0.3) * (1.55 * f + r) + join;
+    if (p == 1 || time < least) {
+      best = p;
+      least = time;
+    }
+  }
+  return best;
+}
+
+DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b, bool alike) {
   DecodePlan p;
   const int group = d.heads / d.kv_heads;
   p.tiles = (group + kTileHeads - 1) / kTileHeads;
@@ -141,10 +164,13 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   const int64_t steps = b.max_len > step ? ((int64_t)b.max_len + step - 1) / step : 1;
   int64_t parts = 1;
   p.waves = 4;
-  if ((int64_t)b.max_len * d.head_dim <= kShortValues) {
+  if ((int64_t)b.max_len * d.head_dim <= short_values(d)) {
     // One part of 8 waves: a step or two for each of them cost less than the join (a sequence of 256 tokens x 32 heads of 128 6.1
-    // us, in two parts of 4 waves 7.7; of 512 8.9 and 8.0; of 512 x 32 heads of 64 5.6 and 7.7).
-    p.waves = b.max_len > step && p.together == 1 ? 8 : 4;
+    // us, in two parts of 4 waves 7.7; of 512 8.9 and 8.0; of 512 x 32 heads of 64 5.6 and 7.7).  In 8 bits twice as many tokens are in a step, and 4
+    // waves do (401 tokens x 32 heads of 128: 6.6 us, 7.1 with 8 waves, 7.4 in two parts; of 700 7.8 and 7.5 in three).
+    p.waves = b.max_len > step && p.together == 1 && !eight_bits(d) ? 8 : 4;
+  } else if (alike && units * p.together <= kJoinCounters) {
+    parts = parts_alike(d, units, steps);
   } else if (units * p.together <= kJoinCounters) {
     // Fewer workgroups than CUs: as many parts as fill the chip once, up to 4,096 tokens each (130,001 tokens x 8 heads: 256
     // workgroups 97 us, 512 100, 1,024 106).  As many without a split: parts of 1,024 tokens, which even out what the lengths differ
@@ -212,11 +238,11 @@ PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
 // The most parts that vq_attn_decode leaves in all tiles together, over batches of no more than n_seqs sequences of up to max_len tokens: those
 // of decode_plan above, with the tiles and the units that such a batch has at most.
 int64_t decode_most_parts(const vq_attn_desc& d, int64_t n_seqs, int64_t max_len) {
-  if (max_len * d.head_dim <= kShortValues) return 0;
+  if (max_len * d.head_dim <= short_values(d)) return 0;
   vq_attn_batch b = {};
   b.n_seqs = b.n_tokens = 65535;   // enough for several tiles to a workgroup, where there are several
   b.max_len = 1;
-  const DecodePlan p = decode_plan(d, b);
+  const DecodePlan p = decode_plan(d, b, false);
   const auto least = [](int64_t tokens) { return tokens < 1 ? 1 : tokens; };
   const int64_t step = part_step(d), steps = (max_len + step - 1) / step, most = steps < kMostParts ? steps : kMostParts;
   const int64_t wide = d.kv_heads * (int64_t)((p.tiles + p.together - 1) / p.together), tiles = n_seqs * d.kv_heads * p.tiles;
@@ -229,7 +255,8 @@ int64_t decode_most_parts(const vq_attn_desc& d, int64_t n_seqs, int64_t max_len
     const int64_t of_many = many * (each < most ? each : most);
     parts = of_many > parts ? of_many : parts;
   }
-  return parts;
+  const int64_t alike = tiles * most < kMostAlike * p.together ? tiles * most : kMostAlike * p.together;   // with a window
+  return alike > parts ? alike : parts;
 }
 
 // The same of vq_attn_prompt: a call has parts where its units are fewer than `enough`, and then up to enough + units / 2 of them; its
@@ -297,7 +324,7 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const vq_att
     const PromptArgs prompt = {a, prompt_plan(*desc, seen), (uint32_t*)workspace, (float*)workspace + kJoinCounters};
     return hip_status(launch_attn_prompt(prompt, desc->head_dim, bf16, (hipStream_t)stream));
   }
-  both.plan = decode_plan(*desc, seen);
+  both.plan = decode_plan(*desc, seen, 2 * (int64_t)seen.max_len <= batch->max_len);
   both.counter = (uint32_t*)workspace;
   both.part = (float*)workspace + kJoinCounters;
   return hip_status(launch_attn_decode(both, desc->head_dim, bf16, (hipStream_t)stream));

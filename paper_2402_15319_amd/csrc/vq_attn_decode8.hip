@@ -11,6 +11,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void decode8_kernel(
 
 struct Kernels {
   static constexpr int kWholeLines = 6, kThreeDim = kThreeDim8;
+  static constexpr bool kEightWaves = false;
   template <bool BF16, int D, bool WHOLE_LINES, int kWaves, int TILES>
   static constexpr auto kernel = decode8_kernel<BF16, D, WHOLE_LINES, kWaves, TILES>;
 };

@@ -530,7 +530,8 @@ void launch_pages(const DecodeArgs& a, dim3 grid, hipStream_t s) {
     if (a.plan.together == 3) return Kernels::template kernel<BF16, D, WHOLE_LINES, 4, 3><<<grid, 256, 0, s>>>(a);
   if constexpr (D <= kTogetherDim) {
     if (a.plan.together == 2) return Kernels::template kernel<BF16, D, WHOLE_LINES, 4, 2><<<grid, 256, 0, s>>>(a);
-    if (a.plan.waves == 8) return Kernels::template kernel<BF16, D, WHOLE_LINES, 8, 1><<<grid, 512, 0, s>>>(a);   // the plan has none for larger heads
+    if constexpr (Kernels::kEightWaves)
+      if (a.plan.waves == 8) return Kernels::template kernel<BF16, D, WHOLE_LINES, 8, 1><<<grid, 512, 0, s>>>(a);   // the plan has none for larger heads
   }
   Kernels::template kernel<BF16, D, WHOLE_LINES, 4, 1><<<grid, 256, 0, s>>>(a);
 }

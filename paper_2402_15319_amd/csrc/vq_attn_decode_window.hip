@@ -11,6 +11,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void decode_window_k
 
 struct Kernels {
   static constexpr int kWholeLines = 5, kThreeDim = kTogetherDim;
+  static constexpr bool kEightWaves = true;
   template <bool BF16, int D, bool WHOLE_LINES, int kWaves, int TILES>
   static constexpr auto kernel = decode_window_kernel<BF16, D, WHOLE_LINES, kWaves, TILES>;
 };

@@ -68,7 +68,7 @@ hipError_t launch_attn_decode(const DecodeArgs& d, int head_dim, bool, hipStream
   const bool e = a.k_scales != nullptr;
   const int step = e ? 64 : 32;      // of a wave
   REQUIRE(p.chunk >= 4 * step && p.chunk % (4 * step) == 0 && p.parts >= 1 && p.parts <= kMostParts);
-  REQUIRE(p.waves == 4 || (p.waves == 8 && p.parts == 1 && head_dim <= kTogetherDim && p.together == 1));
+  REQUIRE(p.waves == 4 || (p.waves == 8 && !e && p.parts == 1 && head_dim <= kTogetherDim && p.together == 1));
   REQUIRE(p.together >= 1 && p.together <= (head_dim > kTogetherDim ? 1 : e && head_dim > kThreeDim8 ? 2 : 3));
   for (int i = 0; i < 8; ++i) {      // what the kernel goes through of a sequence
     const int len = i == 0 ? a.c.max_len : some_length(a.c.max_len);
