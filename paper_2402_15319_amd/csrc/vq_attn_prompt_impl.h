@@ -122,6 +122,10 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   // The same in 8 bits, in two halves.  16 codes of a token's dimensions, or of a dimension's tokens, to a load; of heads of 96 the last 32 dimensions
   // are 8 to a load.
   const int this_lane = lane;
+  // Where a lane's first pieces go: 16 codes of K are pieces 2 lane and 2 lane + 1 of the wave's tokens, one token after another (further ones 16 / (D / 64) tokens
+  // later, whose turn differs from the first token's in bits that those of the first tokens leave out), 16 of V the two of dimension lane.
+  const int swapped = lane >> 2 & 1, k_at0 = 2 * lane + swapped;
+  const int k_place = (k_at0 / (D / 8) * (D / 8) + ((k_at0 % (D / 8)) ^ k_turn<D>(k_at0 / (D / 8)))) * 16, v_place = (2 * lane + (swapped ^ (lane >> 3 & 1))) * 16;
   constexpr int kCodes = D / 64, kFrags = (D + 63) / 64;
   u32x4 k_codes[E4M3 ? kFrags : 1], v_codes[E4M3 ? kFrags : 1];
   float k_scale = 1.f, v_scale = 1.f;
@@ -186,22 +190,21 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
       odd_codes[number] = 1;
     }
     char* to = lds + (2 * team + ((step / TEAMS) & 1)) * kStep + wave * (kHalf / kWaves);
-    auto k_piece = [&](int at, u32x4 v) {   // of 8 dimensions: the at-th of the wave's tokens, one token after another
-      const int r = at / (D / 8), p = at % (D / 8);
-      *reinterpret_cast<u32x4*>(to + (r * (D / 8) + (p ^ k_turn<D>(r))) * 16) = v;
-    };
-    auto v_piece = [&](int d, int h, u32x4 v) { *reinterpret_cast<u32x4*>(to + kHalf + (2 * d + (h ^ ((d >> 3) & 1))) * 16) = v; };
 #pragma unroll
     for (int j = 0; j < kCodes; ++j) {
+      // Of a lane's two pieces every second four lanes write the other one first: 8 lanes then write 128 bytes of different banks.
+      const u32x4 k = swapped ? u32x4{k_codes[j][2], k_codes[j][3], k_codes[j][0], k_codes[j][1]} : k_codes[j];
+      const u32x4 v = swapped ? u32x4{v_codes[j][2], v_codes[j][3], v_codes[j][0], v_codes[j][1]} : v_codes[j];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        k_piece(128 * j + 2 * lane + h, values8<BF16>(k_codes[j][2 * h], k_codes[j][2 * h + 1], k_scale));
-        v_piece(64 * j + lane, h, values8<BF16>(v_codes[j][2 * h], v_codes[j][2 * h + 1], v_scale));
+        *reinterpret_cast<u32x4*>(to + ((k_place ^ 16 * h ^ 16 * (j * 1024 / D & 15)) + 2048 * j)) = values8<BF16>(k[2 * h], k[2 * h + 1], k_scale);
+        *reinterpret_cast<u32x4*>(to + kHalf + ((v_place ^ 16 * h) + 2048 * j)) = values8<BF16>(v[2 * h], v[2 * h + 1], v_scale);
       }
     }
     if constexpr (E4M3 && kFrags > kCodes) {
-      k_piece(128 * kCodes + lane, values8<BF16>(k_codes[kCodes][0], k_codes[kCodes][1], k_scale));
-      v_piece(64 * kCodes + (lane >> 1), lane & 1, values8<BF16>(v_codes[kCodes][0], v_codes[kCodes][1], v_scale));
+      const int at = 128 * kCodes + lane, r = at / (D / 8), d = 64 * kCodes + (lane >> 1);
+      *reinterpret_cast<u32x4*>(to + (r * (D / 8) + ((at % (D / 8)) ^ k_turn<D>(r))) * 16) = values8<BF16>(k_codes[kCodes][0], k_codes[kCodes][1], k_scale);
+      *reinterpret_cast<u32x4*>(to + kHalf + (2 * d + ((lane & 1) ^ ((d >> 3) & 1))) * 16) = values8<BF16>(v_codes[kCodes][0], v_codes[kCodes][1], v_scale);
     }
   };
 
@@ -236,6 +239,10 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     return keep;
   };
 
+  auto next_step = [&](int step) {   // E4M3: while the last products of a step are still under way
+    if (step + TEAMS < steps) store(step + TEAMS);
+    if (step + 2 * TEAMS < steps) fetch(step + 2 * TEAMS);
+  };
   // masked: some row of the wave leaves out some token of the step.  Where it is known only here (WINDOW), both kinds of steps are one stretch of code.
   auto work = [&](int step, auto masked) {
     constexpr bool known = !std::is_same<decltype(masked), bool>::value;
@@ -359,8 +366,6 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   auto turn = [&](int step) {
     if constexpr (E4M3) {
       lds_written();
-      if (step + TEAMS < steps) store(step + TEAMS);
-      if (step + 2 * TEAMS < steps) fetch(step + 2 * TEAMS);
     } else {
       lds_turn();
       if (step + TEAMS < steps) load(step + TEAMS);
@@ -371,8 +376,9 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     for (; step - team < steps; step += TEAMS) {
       turn(step);
       const int at = real(step) * kTokens, end = at + kTokens - 1;
-      if ((TEAMS > 1 && step >= steps) || at > wave_last || (end <= wave_first - a.window && at >= a.sinks)) continue;
-      work(step, !(end <= wave_first && (at > wave_last - a.window || end < a.sinks)));
+      if ((TEAMS == 1 || step < steps) && at <= wave_last && (end > wave_first - a.window || at < a.sinks))
+        work(step, !(end <= wave_first && (at > wave_last - a.window || end < a.sinks)));
+      if constexpr (E4M3) next_step(step);
     }
   } else {
   // First the steps whose tokens all of the wave's rows attend.
