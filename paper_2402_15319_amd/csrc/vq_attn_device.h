@@ -95,13 +95,10 @@ template <bool BF16> __device__ __forceinline__ u32x4 pack8(f32x8 p) {
   else return __builtin_bit_cast(u32x4, __builtin_convertvector(p, f16x8));
 }
 
-// The larger, and the smaller, of each two halves, as integers: of magnitudes, the larger or smaller number.
+// The larger of each two halves, as integers: of magnitudes, the larger number.
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
-__device__ __forceinline__ uint32_t smaller2(uint32_t a, uint32_t b) {
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
 
 // Eight codes (e4m3, two dwords) as values of the cache's type: exactly, for a block's scale is a power of two that leaves every code a
@@ -143,6 +140,8 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t voff, uin
 __device__ __forceinline__ void lds_turn() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
+
+__device__ __forceinline__ void lds_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }   // the wave's own loads
 
 // The same where nothing comes into LDS past the registers: the wave's writes to LDS and reads from it are done, its loads stay under way.
 __device__ __forceinline__ void lds_written() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }

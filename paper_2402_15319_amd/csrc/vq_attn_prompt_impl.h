@@ -34,7 +34,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   constexpr int KS = D / 16, DT = D / 32, kLoads = D / 32;     // loads of a wave for its 16 tokens' K, and for their V
   constexpr int kHalf = kTokens * D * 2, kStep = 2 * kHalf;    // bytes of K, or V, of a step
   __shared__ __attribute__((aligned(1024))) char lds[TEAMS * 2 * kStep];
-  __shared__ uint32_t odd_codes[kWaves * TEAMS];   // E4M3: values that are no numbers, by the waves that brought them
+  __shared__ uint32_t odd_values[WINDOW ? kWaves * TEAMS : 1];   // values that are no numbers and were taken out, by the waves that did
   const int tid = threadIdx.x, number = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = number % kWaves, team = number / kWaves;
   // The heads are neighbours, and so are on the 8 XCDs in turn: those of an XCD keep to their keys and values.  Of the tiles the last come
@@ -187,7 +187,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
       for (int j = 0; j < (E4M3 ? kFrags : 1); ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) v_codes[j][e] &= ~((odd(v_codes[j][e]) >> 7) * 0xffu);
-      odd_codes[number] = 1;
+      odd_values[number] = 1;
     }
     char* to = lds + (2 * team + ((step / TEAMS) & 1)) * kStep + wave * (kHalf / kWaves);
 #pragma unroll
@@ -209,8 +209,8 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   };
 
   int step = begin + team;
+  if constexpr (WINDOW) odd_values[number] = 0;
   if constexpr (E4M3) {
-    odd_codes[number] = 0;
     if (step < steps) {
       fetch(step);
       store(step);
@@ -239,6 +239,35 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     return keep;
   };
 
+  // 16 bits, WINDOW: takes out of the step's values in LDS what is no number.  Another wave that is at the same does the same; one whose rows all see the
+  // step may read it before or after, and finds the word of it behind its last step.
+  auto values_in_lds = [&](int step) {
+    return reinterpret_cast<u32x4*>(lds + (2 * team + ((step / TEAMS) & 1)) * kStep + kHalf) + apart(this_lane);
+  };
+  auto clear_odd = [&](int step) {
+    u32x4* vt = values_in_lds(step);
+    odd_values[number] = 1;
+#pragma unroll 1
+    for (int n = 0; n < kHalf / 16; n += 64) {
+      u32x4 v = vt[n];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] &= ~odd_halves<BF16>(v[i]);
+      vt[n] = v;
+    }
+  };
+  // The same of the wave's own tokens that no row sees, whatever they are, before anybody reads them.
+  auto clear_unseen = [&](int step) {
+    const int lane = apart(this_lane), at0 = real(step) * kTokens + 16 * wave;
+    u32x4* vt = values_in_lds(step) + wave * (kHalf / kWaves / 16);
+#pragma unroll
+    for (int n = 0; n < kHalf / kWaves / 16; n += 64) {
+      const int d = (n + lane) / 2, at = at0 + 8 * ((lane & 1) ^ (d >> 3 & 1));
+      u32x4 keep = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) keep[i / 2] |= at + i < len && (at + i < a.sinks || at + i >= first_seen) ? 0xffffu << (i % 2 * 16) : 0u;
+      vt[n] &= keep;
+    }
+  };
   auto next_step = [&](int step) {   // E4M3: while the last products of a step are still under way
     if (step + TEAMS < steps) store(step + TEAMS);
     if (step + 2 * TEAMS < steps) fetch(step + 2 * TEAMS);
@@ -337,25 +366,16 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
       for (int at = 0; at < 4 * DT; at += kBatch) {
         if (at > 0) v_batch(at);
         if (!E4M3 && !known && masked) {
-          // To the same end every magnitude is brought to the largest finite one, and whether that changes a token that some row may see is
-          // looked at on the way: half the instructions.  (What such a value then adds to a row that sees it, infinity or NaN makes away with.)
-          const int first = real(step) * kTokens;
-          const bool clear = first + kTokens > len || (first < first_seen && first + kTokens > a.sinks);
-          uint32_t size = 0;   // the largest magnitudes of both halves, as integers
+          // To the same end a product with zeros (of any order: each value meets one) says whether there is a value at all that is no number, in place of
+          // hundreds of instructions that look at each; then it is cleared in LDS.
+          f32x4 none = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < kBatch / DT; ++c) {
-            u32x4 keep = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
-            if (clear) keep &= up_to_last(apart(first + 16 * (at / DT + c)));
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t v = f[c * DT + i][e];
-                size = larger2(size, v & keep[e]);
-                f[c * DT + i][e] = (v & 0x80008000u) | smaller2(v & 0x7fff7fffu, BF16 ? 0x7f7f7f7fu : 0x7bff7bffu);
-              }
+          for (int j = 0; j < kBatch; ++j) none = mfma16<BF16>(f[j], u32x4{0, 0, 0, 0}, none);
+          const float any = (none[0] + none[1]) + (none[2] + none[3]);
+          if (__builtin_expect(__any(__builtin_isunordered(any, any)), 0)) {
+            clear_odd(step);
+            v_batch(at);
           }
-          left_out |= odd_halves<BF16>(size);
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) o[(at + j) % DT] = mfma32<BF16>(f[j], p[(at + j) / DT], o[(at + j) % DT]);
@@ -367,6 +387,13 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     if constexpr (E4M3) {
       lds_written();
     } else {
+      if constexpr (WINDOW) {
+        const int at = real(step) * kTokens + 16 * wave;
+        if (step < steps && (at + 16 > len || (at < first_seen && at + 16 > a.sinks))) {
+          lds_arrived();
+          clear_unseen(step);
+        }
+      }
       lds_turn();
       if (step + TEAMS < steps) load(step + TEAMS);
     }
@@ -401,9 +428,9 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) largest = __builtin_elementwise_maximum(largest, o[i][j]);   // NaN where one of them is
-  if constexpr (E4M3) {
+  if constexpr (WINDOW) {
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) left_out |= odd_codes[kWaves * team + i];
+    for (int i = 0; i < kWaves; ++i) left_out |= odd_values[kWaves * team + i];
   }
   if (__builtin_expect(__any(left_out != 0 || (__builtin_isunordered(largest, largest) && !__builtin_isunordered(l, l))), 0)) {
 #pragma unroll

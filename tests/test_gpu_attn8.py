@@ -279,3 +279,34 @@ def test_a_prompt_is_what_its_tokens_are_one_at_a_time(bits):
     torch.cuda.synchronize()
     assert (np.abs((got - out).double().cpu().numpy()) <= 2 * b_out).all()
     assert (np.abs((got_lse - lse).double().cpu().numpy()) <= 2 * b_lse).all()
+
+
+@pytest.mark.parametrize("bits, value", [(16, float("nan")), (16, float("inf")), (8, float("nan"))])
+@pytest.mark.parametrize("heads, kv, dim", [(2, 2, 64), (4, 1, 128), (2, 1, 96), (1, 1, 256)])
+def test_what_is_no_number_in_long_prompts_with_a_window(heads, kv, dim, bits, value):
+    """Steps that some waves' rows see whole and others in part, or not at all: it goes to the rows that see it, and every other row is what it is
+    without it, bit for bit."""
+    import torch
+    from cache8_cases import join8, split8
+    for window, sinks in ((150, 0), (70, 100)):
+        p = Windowed(heads, kv, dim, 16, "f16", [420], [420], seed=8, bits=bits, window=window, sinks=sinks)
+        clean = run_window(p, "prompt")
+        for token in (3, 99, 130, 200, 319, 419):
+            page, slot = int(p.table[0, token // 16]), token % 16
+            if bits == 8:
+                c, s = split8(p.desc, p.v_pages, False)
+                c = c.copy()
+                was = p.v_pages
+                c[page, 0, 5, slot] = 0x7f
+                p.v_pages = join8(c, s)
+            else:
+                was = p.v_pages.clone()
+                p.v_pages[page, 0, 5, slot] = value
+            out, lse = run_window(p, "prompt")
+            p.v_pages = was
+            rows = torch.arange(420, device=out.device)
+            sees = (rows >= token) & ((rows < token + window) | (token < sinks))
+            reads = torch.arange(heads, device=out.device) < heads // kv
+            hit = (sees[:, None] & reads)[..., None] & (torch.arange(dim, device=out.device) == 5)
+            assert bool((torch.isnan(out[hit]) if value != value else out[hit] == value).all())
+            assert torch.equal(out[~hit], clean[0][~hit]) and torch.equal(lse, clean[1])
