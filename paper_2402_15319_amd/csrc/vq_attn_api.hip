@@ -190,9 +190,9 @@ DecodePlan decode_plan(const vq_attn_desc& d, const vq_attn_batch& b, bool alike
 }
 
 constexpr int kLeastSteps = 8;          // of a part
-constexpr int64_t kOneTeamUnits = 512, kWideUnits = 448;   // workgroups that the chip runs at once, or nearly: of one team, and of heads of 256
+constexpr int64_t kOneTeamUnits = 512, kWideUnits = 448, kSmallUnits = 768;   // workgroups that the chip runs at once, or nearly: of one team, of heads of 256, and of heads of 64
 
-PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
+PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b, bool window) {
   PromptPlan p;
   // The heads of a tile: as few tiles as sequences of the mean length need; 4, 2 or 1, with 32 successive tokens of a head to a wave, if that
   // takes no more than an eighth more of them.  (Nine prompts of up to 2,500 x 8 key/value heads, 4 heads to each: 98 us with four
@@ -225,7 +225,9 @@ PromptPlan prompt_plan(const vq_attn_desc& d, const vq_attn_batch& b) {
   p.teams = d.head_dim <= 128 && (lone || few) ? 2 : 1;
   // Parts, where they bring the workgroups near to what the chip runs at once (heads of 256 have one workgroup to a compute unit, and of
   // longer parts: 16 heads, 1,500 and 2,048 tokens 67 and 88 us whole, 51 and 80 in two parts).
-  const int64_t enough = p.teams == 2 ? kEnoughUnits : d.head_dim > 128 ? kWideUnits : kOneTeamUnits;
+  // Three workgroups on heads of 64 share a compute unit: with a window, and over pages in 8 bits, the parts go by that (chunks of 515 behind 12,000 tokens, 32
+  // heads on 8: four parts 42.7 us, three 50.0; without a window 83 and 95).  Other calls keep the parts that they had, and with them their bits.
+  const int64_t enough = p.teams == 2 ? kEnoughUnits : d.head_dim > 128 ? kWideUnits : d.head_dim == 64 && (window || eight_bits(d)) ? kSmallUnits : kOneTeamUnits;
   int64_t parts = units < enough ? (enough + units / 2) / units : 1;
   while (parts > 1 && parts * parts > steps) --parts;   // to join a part takes about as long as a step
   int64_t per = (steps + parts - 1) / parts;
@@ -262,7 +264,7 @@ int64_t decode_most_parts(const vq_attn_desc& d, int64_t n_seqs, int64_t max_len
 // The same of vq_attn_prompt: a call has parts where its units are fewer than `enough`, and then up to enough + units / 2 of them; its
 // units are at most those of tiles of 64 rows and two tiles of one row's heads for each sequence.
 int64_t prompt_most_parts(const vq_attn_desc& d, int64_t n_seqs, int64_t n_tokens, int64_t max_len) {
-  const int64_t steps = (max_len + kPromptTokens - 1) / kPromptTokens, enough = d.head_dim > 128 ? kWideUnits : kOneTeamUnits;
+  const int64_t steps = (max_len + kPromptTokens - 1) / kPromptTokens, enough = d.head_dim > 128 ? kWideUnits : d.head_dim == 64 ? kSmallUnits : kOneTeamUnits;
   const int64_t of_steps = (steps + kLeastSteps - 1) / kLeastSteps, of_join = (int64_t)sqrt((double)steps);   // steps below 2^24: exact
   const int64_t each = of_steps < of_join ? of_steps : of_join;
   if (each <= 1) return 0;
@@ -321,7 +323,7 @@ int attn_impl(const vq_attn_desc* desc, const vq_attn_batch* batch, const vq_att
   seen.max_len = (int32_t)(decode ? decode_seen(*desc, batch->max_len, window) : prompt_seen(batch->max_len, window));
   const bool bf16 = desc->dtype == VQ_BF16;
   if (!decode) {
-    const PromptArgs prompt = {a, prompt_plan(*desc, seen), (uint32_t*)workspace, (float*)workspace + kJoinCounters};
+    const PromptArgs prompt = {a, prompt_plan(*desc, seen, window != nullptr), (uint32_t*)workspace, (float*)workspace + kJoinCounters};
     return hip_status(launch_attn_prompt(prompt, desc->head_dim, bf16, (hipStream_t)stream));
   }
   both.plan = decode_plan(*desc, seen, 2 * (int64_t)seen.max_len <= batch->max_len);
