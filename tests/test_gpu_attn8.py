@@ -310,3 +310,32 @@ def test_what_is_no_number_in_long_prompts_with_a_window(heads, kv, dim, bits, v
             hit = (sees[:, None] & reads)[..., None] & (torch.arange(dim, device=out.device) == 5)
             assert bool((torch.isnan(out[hit]) if value != value else out[hit] == value).all())
             assert torch.equal(out[~hit], clean[0][~hit]) and torch.equal(lse, clean[1])
+
+
+@pytest.mark.parametrize("call", ["decode", "prompt"])
+@pytest.mark.parametrize("bits, dim, page", [(8, 128, 64), (16, 256, 128), (8, 256, 16), (16, 64, 16)])
+def test_pages_beyond_4_gib(bits, dim, page, call):
+    """The last pages of a large cache: bit for bit what the same tokens give in a small one."""
+    import torch
+    from cache8_cases import split8
+    p = Windowed(16, 16, dim, page, "f16", [400, 33], None if call == "decode" else [70, 33], seed=2, bits=bits, window=150, sinks=20)
+    out, lse = check(p, call)
+    few, by_page = p.n_pages, 16 * page * dim * bits // 8
+    many = 2 ** 32 // by_page + few + 3
+
+    def put(small, by_slot):
+        if bits == 16:
+            big = torch.zeros(many, *small.shape[1:], dtype=small.dtype, device=small.device)
+            big[many - few:] = small
+            return big
+        codes, scales = (torch.from_numpy(np.ascontiguousarray(x)).to(small.device).view(torch.uint8).flatten() for x in split8(p.desc, small, by_slot))
+        big = torch.zeros(many * (by_page + page * 4), dtype=torch.uint8, device=small.device)
+        big[(many - few) * by_page:many * by_page] = codes
+        big[len(big) - len(scales):] = scales
+        return big
+
+    p.k_pages, p.v_pages = put(p.k_pages, True), put(p.v_pages, False)
+    p.desc.n_pages = many
+    p.table_d.add_(many - few)
+    far, far_lse = run_window(p, call)
+    assert torch.equal(far, out) and torch.equal(far_lse, lse)
