@@ -73,8 +73,10 @@ __device__ __forceinline__ int64_t head_of(const CacheArgs& c, int s, int pos, i
 
 constexpr int octets(int d) { return d == 64 ? 8 : d == 256 ? 32 : 16; }   // lanes for a head's dimensions, 8 each (of 16, those of 96 leave 4 idle)
 
-// Few new tokens for each sequence: the threads of a token take eight dimensions of a head's key and value each.  They look at the block's other new tokens,
-// if there are any, for its scale; those of the first one also see to the earlier tokens' codes, where the scale grows, and to the scale.  (Another token's
+// Few new tokens for each sequence: the threads of a token take eight dimensions of a head's key and value each.  What bounds it is the way through
+// the sequences' lengths, the table and the scale to the first store (one token of 8 sequences x 8 heads: 3.8 us, of 64
+// 4.0), and for hundreds of tokens the values' single bytes, 16 or more apart (512 sequences x 8 heads: 8.6 us, 3 MB).  The threads look at the block's other
+// new tokens, if there are any, for its scale; those of the first one also see to the earlier tokens' codes, where the scale grows, and to the scale.  (Another token's
 // threads may find the new scale in place of the old one: theirs is the same from either.)
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void append8_few_kernel(const AppendArgs a) {
@@ -155,14 +157,21 @@ __global__ __launch_bounds__(256) void append8_few_kernel(const AppendArgs a) {
   }
 }
 
-// Any number of new tokens: a workgroup takes 64 positions of a sequence and a head, half of its waves the keys and half the values, a wave 64 of the
-// dimensions, a lane eight positions by eight dimensions in registers.  The lanes and waves that have a block exchange their largest magnitudes.  Loads
-// are 16 bytes along whatever is contiguous in the source, 128 in a row of lanes, stores 8 along what is in the page; in between the lane turns its block where
-// those differ.
+// Any number of new tokens: a workgroup takes 64 positions of a sequence and a head, half of its waves the keys and half the values, a lane eight positions by
+// eight dimensions in registers.  Where the source runs along positions a wave takes all of them and 64 dimensions, otherwise all dimensions of as many positions
+// as it has lanes for.  The lanes, and in the first case the waves, that have a block exchange their largest magnitudes.  Loads are 16 bytes along whatever is
+// contiguous in the source, 128 or more in a row of lanes; the lane turns its block where the page runs along the other; values' codes of whole blocks
+// go through LDS to the lane that stores a dimension's 16 at once, successive dimensions in successive lanes.  Memory bounds it (11,700 tokens x 32 heads of
+// 128, pages of 16, 287 MB: rows whole 61 us, 4.7 TB/s, and 67 with values stored 8 bytes by 8 from where they are; a conversion of as many bytes in order 51.  In
+// the order of the batched product 76, 64 where sequences begin at multiples of 64 in the source and in the page: lines are read in two halves otherwise, and odd
+// numbers cost 16-byte loads their alignment).  8 waves to a SIMD, loads past the caches (85 us) or stores past them do no better.  16 positions in place of 64 (a
+// block to a lane) reads half lines: 44 us for 32 tokens of one sequence, 6 with 64.
 constexpr int kTile8 = 64;
 template <bool BF16, int D>
 __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append8_kernel(const AppendArgs a) {
   constexpr int kParts = (D + 63) / 64;   // waves for the dimensions
+  constexpr int kLanes = octets(D);        // that share a position, where the source runs along dimensions
+  __shared__ u32x4 codes_of[kParts][256];  // of values
   __shared__ uint32_t of_blocks[2 * kParts][kTile8 / kBlock];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool values = wave >= kParts;
@@ -176,11 +185,11 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append8_kernel(const Ap
   // lanes: positions first where the source runs along them, dimensions first where it runs along those
   const Strides st = values ? a.vs : a.ks;
   const bool along_tokens = st.token == 1 && st.dim != 1;
-  const int x = along_tokens ? lane & 7 : lane >> 3, y = along_tokens ? lane >> 3 : lane & 7;
+  const int x = along_tokens ? lane & 7 : wave % kParts * (64 / kLanes) + lane / kLanes, y = along_tokens ? lane >> 3 : lane % kLanes;
   const int pos = tile0 + 8 * x, block0 = pos & -kBlock;
   // Its dimensions: 8 y .. + 7, or, where nothing is turned, every eighth from y, so that the lanes of an instruction have successive ones.
   const bool spread = D % 64 == 0 && values && along_tokens;
-  const int d = 64 * (wave % kParts) + (spread ? y : 8 * y), d_step = spread ? 8 : 1;
+  const int d = (along_tokens ? 64 * (wave % kParts) : 0) + (spread ? y : 8 * y), d_step = spread ? 8 : 1;
   const int64_t dim = st.dim * d_step;
   // Of its positions lo .. hi - 1 are new and have a place, and those before `kept` hold earlier tokens of the block.
   const bool mine = d < D && block0 < stop && block0 + kBlock > from;
@@ -219,16 +228,16 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append8_kernel(const Ap
     most = other > most ? other : most;
   };
   // the lanes with the block's other positions and the wave's other dimensions, then the waves with other dimensions
-  exchange(1);
-  exchange(8);
   if (along_tokens) {
+    exchange(1);
+    exchange(8);
     exchange(16);
     exchange(32);
   } else {
-    exchange(2);
-    exchange(4);
+#pragma unroll
+    for (int w = 1; w <= kLanes; w *= 2) exchange(w);
   }
-  if constexpr (kParts > 1) {
+  if (kParts > 1 && along_tokens) {
     if (y == 0) of_blocks[wave][x >> 1] = most;   // (two lanes, the same number)
     __syncthreads();
 #pragma unroll
@@ -261,7 +270,19 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append8_kernel(const Ap
   } else {
     uint8_t* to = reinterpret_cast<uint8_t*>(a.v_pages) + (head << a.c.page_shift) * D + ((int64_t)d << a.c.page_shift) + slot;
     const int step = d_step * size;
-    if (whole) {
+    if (!along_tokens && D % 64 == 0 && __ballot(block0 >= from && block0 + kBlock <= stop) == ~0ull) {   // (lanes that have left count as 0)
+      u32x4* room = &codes_of[wave - kParts][0];   // [block of the wave][dimension], an octet of dimensions turned by its number, which spreads them over the banks
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<u32x2*>(reinterpret_cast<char*>(room + lane / (2 * kLanes) * D + d + ((i + y) & 7)) + (x & 1) * 8) = codes8<BF16>(in[i], scale);
+      asm volatile("" ::: "memory");   // (a wave's own LDS operations are in order)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = 64 * j + lane, b = at / D, e = at % D, dim = (e & -8) + ((e - (e >> 3)) & 7);
+        const int64_t base = __shfl((int64_t)(head << a.c.page_shift) * D + (slot & -kBlock), b * 2 * kLanes);
+        *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(a.v_pages) + base + ((int64_t)dim << a.c.page_shift)) = room[at];
+      }
+    } else if (whole) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x2*>(to + i * step) = codes8<BF16>(in[i], scale);
     } else if (lo < hi || grows) {   // other tokens' slots stay as they are
@@ -289,8 +310,11 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append8_kernel(const Ap
 
 template <bool BF16, int D>
 hipError_t launch_dim(const AppendArgs& a, hipStream_t s) {
-  // Few new tokens for each sequence: most of a tile would be empty.
-  if (!a.c.q_start || a.c.n_tokens <= 2 * (int64_t)a.c.n_seqs)
+  // Few new tokens for each sequence: most of a tile would be empty, but each of them goes through the block's others.  (64 sequences x 32 heads of 128, rows
+  // whole: one new token each 5.7 us, 13.0 in tiles; four 16.3 and 14.0.  In the order of the batched product: one 8.4 and 18.8; two 14.6 and 19.8; three 27.5
+  // and 21.7.  512 sequences x 8 heads, rows whole: four 28.5 and 35.8; in the order of the product two 23.7 and 49.5, four 69.7 and 52.6.)
+  const int few = a.ks.dim == 1 && a.vs.dim == 1 ? 3 : 2;
+  if (!a.c.q_start || a.c.n_tokens <= few * (int64_t)a.c.n_seqs)
     append8_few_kernel<BF16, D><<<dim3(a.c.n_tokens, (a.c.kv_heads * octets(D) + 255) / 256), 256, 0, s>>>(a);
   else
     append8_kernel<BF16, D><<<(unsigned)((a.c.n_tokens / kTile8 + 2 * (int64_t)a.c.n_seqs) * a.c.kv_heads), 128 * ((D + 63) / 64), 0, s>>>(a);
