@@ -183,8 +183,9 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append8_kernel(const Ap
   const int tile0 = (from / kTile8 + tile.number) * kTile8;
   if (last <= first || from >= stop || tile0 >= stop) return;        // no new token: for the whole workgroup
   // lanes: positions first where the source runs along them, dimensions first where it runs along those
+  const auto along = [](const Strides& st) { return st.token == 1 && st.dim != 1; };
   const Strides st = values ? a.vs : a.ks;
-  const bool along_tokens = st.token == 1 && st.dim != 1;
+  const bool along_tokens = along(st);
   const int x = along_tokens ? lane & 7 : wave % kParts * (64 / kLanes) + lane / kLanes, y = along_tokens ? lane >> 3 : lane % kLanes;
   const int pos = tile0 + 8 * x, block0 = pos & -kBlock;
   // Its dimensions: 8 y .. + 7, or, where nothing is turned, every eighth from y, so that the lanes of an instruction have successive ones.
@@ -237,14 +238,15 @@ __global__ __launch_bounds__(128 * ((D + 63) / 64)) void append8_kernel(const Ap
 #pragma unroll
     for (int w = 1; w <= kLanes; w *= 2) exchange(w);
   }
-  if (kParts > 1 && along_tokens) {
+  if (kParts > 1 && (along(a.ks) || along(a.vs))) {   // the same for all of the workgroup's waves, which meet here
     if (y == 0) of_blocks[wave][x >> 1] = most;   // (two lanes, the same number)
     __syncthreads();
+    if (along_tokens)
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-      const uint32_t other = of_blocks[(values ? kParts : 0) + i][x >> 1];
-      most = other > most ? other : most;
-    }
+      for (int i = 0; i < kParts; ++i) {
+        const uint32_t other = of_blocks[(values ? kParts : 0) + i][x >> 1];
+        most = other > most ? other : most;
+      }
   }
   if (head < 0) return;
   const float scale = fmaxf(scale_for<BF16>(most), old);

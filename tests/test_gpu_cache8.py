@@ -197,6 +197,35 @@ def test_many_sequences(new, layout):
     pages.compare(kp, vp, pages.want(k, v))
 
 
+@pytest.mark.parametrize("k_layout, v_layout", [("tokens", "features"), ("features", "tokens"), ("features", "odd"), ("odd features", "heads")])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+def test_keys_and_values_in_different_orders(dim, k_layout, v_layout):
+    for page, lens, new in ((16, [100, 200, 7], [64, 200, 7]), (64, [300, 65], [177, 64]), (32, [20, 40, 9], [2, 1, 2])):
+        p = Problem(3, 3, dim, page, "f16", lens, new, seed=dim)
+        pages = Pages(p)
+        k, v = _values(p, 11), _values(p, 12)
+        kp, vp = pages.buffers()
+        p.layout = k_layout
+        k_rows = p.rows(k, 3)
+        p.layout = v_layout
+        _append(p, k_rows, p.rows(v, 3), kp, vp)
+        pages.compare(kp, vp, pages.want(k, v))
+
+
+@pytest.mark.parametrize("layout", ["tokens", "features"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_one_long_sequence_among_many_without_new_tokens(dtype, layout):
+    """Few tokens for each sequence on the average: those of the long one still make their blocks' scales together."""
+    new = [0] * 150 + [301] + [1, 0, 3] * 10
+    lens = [n + (5 * i) % 40 for i, n in enumerate(new)]
+    p = Problem(2, 2, 128, 32, dtype, lens, new, layout=layout, seed=4)
+    pages = Pages(p, loud=2.0 ** -4)
+    k, v = _values(p, 13), _values(p, 14)
+    kp, vp = pages.buffers()
+    _append(p, p.rows(k, 2), p.rows(v, 2), kp, vp)
+    pages.compare(kp, vp, pages.want(k, v))
+
+
 def test_a_captured_graph_and_another_stream():
     """A graph follows the lengths and the table when it is replayed."""
     import torch
