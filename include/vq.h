@@ -298,7 +298,7 @@ typedef struct vq_attn_desc {
   int32_t head_dim;     /* 64, 96, 128 or 256                                         */
   int32_t page_size;    /* tokens in a page: 16, 32, 64 or 128                        */
   int32_t n_pages;      /* pages in a K or V buffer                                   */
-  int32_t dtype;        /* VQ_F16 or VQ_BF16: q, k, v, the cache and out              */
+  int32_t dtype;        /* VQ_F16 or VQ_BF16: q, k, v, out, and the cache if cache_dtype is 0 */
   float scale;          /* of the logits: positive, at most 2.35e38 (scale * log2(e) is
                            finite), as 1 / sqrt(head_dim)                             */
   union {
@@ -355,7 +355,7 @@ typedef struct vq_attn_window { int32_t window, sinks; } vq_attn_window;
 VQ_API int vq_cache_bytes(const vq_attn_desc* desc, size_t* bytes);
 
 /*
- * The new tokens' keys and values into their pages, copied bit for bit; k and v are
+ * The new tokens' keys and values into their pages, copied bit for bit (pages in 8 bits: rounded as above); k and v are
  * [n_tokens][kv_heads][head_dim] with the strides given.  Tokens with a negative position, with one
  * of max_len or more, or in a page outside the cache, are left out.  k_pages and v_pages are 16-byte aligned; the arrays do
  * not overlap.  desc->scale is not used.  One launch.
