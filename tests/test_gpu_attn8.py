@@ -339,3 +339,25 @@ def test_pages_beyond_4_gib(bits, dim, page, call):
     p.table_d.add_(many - few)
     far, far_lse = run_window(p, call)
     assert torch.equal(far, out) and torch.equal(far_lse, lse)
+
+
+@pytest.mark.parametrize("bits, window", [(8, None), (8, 40), (16, 40)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_rows_behind_the_last_sequence(dim, bits, window):
+    """A padded batch: q_start ends before n_tokens, and the rows from there on stay as they were."""
+    import torch
+    import paper_2402_15319_amd as vq
+    p = Windowed(4, 2, dim, 16, "f16", [70, 300, 9], [70, 33, 2], seed=6, bits=bits, window=window, sinks=3)
+    out, lse = check(p, "prompt")
+    for more in (1, 200):
+        pad = lambda t, x: torch.cat([t, torch.full((more, *t.shape[1:]), x, dtype=t.dtype, device=t.device)])  # noqa: E731
+        batch = vq.AttnBatch(p.lens_d, p.table_d, n_tokens=p.total + more, max_len=300, q_start=p.start_d)
+        o, e = pad(torch.empty_like(out), 55.0), pad(torch.empty_like(lse), 55.0)
+        args = pad(p.q, float("nan")), p.k_pages, p.v_pages, o, vq.attn_workspace(p.desc, batch)
+        if window is None:
+            vq.vq_attn_prompt(p.desc, batch, *args, lse=e)
+        else:
+            vq.vq_attn_prompt_window(p.desc, batch, vq.VQAttnWindow(window, 3), *args, lse=e)
+        torch.cuda.synchronize()
+        p.check(o[:p.total], e[:p.total])
+        assert bool((o[p.total:] == 55).all()) and bool((e[p.total:] == 55).all())

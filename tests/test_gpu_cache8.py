@@ -226,6 +226,24 @@ def test_one_long_sequence_among_many_without_new_tokens(dtype, layout):
     pages.compare(kp, vp, pages.want(k, v))
 
 
+@pytest.mark.parametrize("new", [[1, 2, 0], [70, 33, 2]])
+@pytest.mark.parametrize("layout", ["tokens", "features"])
+def test_rows_behind_the_last_sequence(layout, new):
+    """A padded batch: q_start ends before n_tokens, and the rows from there on go nowhere."""
+    import torch
+    import paper_2402_15319_amd as vq
+    p = Problem(2, 2, 128, 16, "f16", [70, 300, 9], new, layout=layout, seed=6)
+    pages = Pages(p)
+    k, v = _values(p, 15), _values(p, 16)
+    want = pages.want(k, v)
+    pad = lambda t: torch.cat([t, torch.full((2, *t.shape[1:]), float("nan"), dtype=t.dtype)])  # noqa: E731
+    kp, vp = pages.buffers()
+    batch = vq.AttnBatch(p.lens_d, p.table_d, n_tokens=p.total + 2, max_len=300, q_start=p.start_d)
+    vq.vq_cache_append(p.desc, batch, p.rows(pad(k), 2), p.rows(pad(v), 2), kp, vp)
+    torch.cuda.synchronize()
+    pages.compare(kp, vp, want)
+
+
 def test_a_captured_graph_and_another_stream():
     """A graph follows the lengths and the table when it is replayed."""
     import torch
