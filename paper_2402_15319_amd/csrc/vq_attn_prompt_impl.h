@@ -26,8 +26,11 @@ template <int D> __device__ __forceinline__ int k_turn(int r) {
 // E4M3: pages in 8 bits.  A wave's 16 tokens are one block; their codes come into registers while the step before the one before is worked on, and go
 // to LDS as values of the type (exactly), each once for the workgroup, so that the products are those of 16 bits.  Tokens that no row sees and
 // values that are no numbers stay behind on the way, so that no step looks for them again.
-// WINDOW: a.window and a.sinks.  What no row of the tile sees between the sinks and the window, in whole steps, is passed over: `step` counts the
-// steps that are gone through, real(step) is the place of one in the sequence.
+// WINDOW: a.window and a.sinks.  What no row of the tile sees between the sinks and the window is passed over: in 16 bits in whole sixteens of tokens, each
+// one wave's loads of a step, where that takes a step less than in whole steps (grains, below).  Grains are counted as they are gone through; place(number
+// of one) is where it begins in the sequence.  Sinks are then an even number of sixteens, so that the 32 tokens of half a step are neighbours.  (In whole steps, 4 sinks take
+// a step of their own: 5,000 tokens, 32 heads on 8, window 1,024 106.7 us, 102.7 so; 4,000 tokens, window 64 34.6 and 28.5, 256 44.2 and 38.3.  Nine prompts without sinks,
+// window 333, pay 1.4 of 78 us for it.  In 8 bits the steps stay whole: it would be in the way of the registers, 4,096 tokens 161 and 165.)
 template <bool BF16, int D, int TEAMS, bool E4M3, bool WINDOW>
 __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   const AttnArgs& a = A.a;
@@ -57,16 +60,27 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   const bool valid = row + col <= end && token_in < n;
   const int most = behind + (token0 + tokens < n ? token0 + tokens : n) - 1;   // highest position of the tile
   const int pos = behind + token, wave_first = behind + low, wave_last = low < n ? behind + high : -1;
-  // The first token in a window of the tile; steps sink_steps .. sink_steps + skip - 1 are passed over.
-  int first_seen = 0, sink_steps = 0, skip = 0;
+  // The first token in a window of the tile; grains sinks_end .. sinks_end + skip - 1 are passed over.
+  constexpr int kGrain = E4M3 ? kTokens : 16, kOfStep = kTokens / kGrain;
+  int first_seen = 0, sinks_end = 0, skip = 0, all = most < 0 ? 0 : (uint32_t)most / kTokens + 1;   // steps of the tile
   if constexpr (WINDOW) {
     first_seen = behind + token0 - a.window + 1 > 0 ? behind + token0 - a.window + 1 : 0;
-    sink_steps = a.sinks < first_seen ? (a.sinks + kTokens - 1) / kTokens : first_seen / kTokens;
-    skip = first_seen / kTokens - sink_steps;
-    skip = skip > 0 ? skip : 0;
+    auto pass_over = [&](uint32_t unit, uint32_t sinks_unit) {   // where that takes fewer steps
+      const int sinks = ((uint32_t)a.sinks + sinks_unit - 1) / sinks_unit * (sinks_unit / kGrain), over = (uint32_t)first_seen / unit * (unit / kGrain) - sinks;
+      if (over <= 0 || most < 0) return;
+      const int rest = ((uint32_t)most / kGrain - over) / kOfStep + 1;
+      if (rest >= all) return;
+      sinks_end = sinks;
+      skip = over;
+      all = rest;
+    };
+    pass_over(kTokens, kTokens);
+    if constexpr (!E4M3) pass_over(16, 32);
   }
-  auto real = [&](int step) { return WINDOW && step >= sink_steps ? step + skip : step; };
-  const int all = most < 0 ? 0 : most / kTokens + 1 - skip;   // steps of the tile, and this part's: begin .. steps - 1
+  // Where a grain begins, the wave's own tokens of a step, and half of a step's.
+  auto place = [&](int grain) { return kGrain * (WINDOW && grain >= sinks_end ? grain + skip : grain); };
+  auto own_place = [&](int step) { return E4M3 ? place(step) + 16 * wave : place(kOfStep * step + wave); };
+  auto half_place = [&](int step, int t) { return E4M3 ? place(step) + 32 * t : place(kOfStep * step + 2 * t); };
   const int begin = blockIdx.y * A.plan.steps, steps = all - begin < A.plan.steps ? all : begin + A.plan.steps;
   if (begin >= all && begin > 0) return;
 
@@ -86,7 +100,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   const int32_t* table = a.c.table + (int64_t)s * a.c.table_width;
   // Lane i: the wave's page in the i-th (mod 64) of the steps that are being loaded; asked for before q, which the loads need not wait for.
   auto pages_from = [&](int step) {
-    const int j = (real(step + TEAMS * lane) * kTokens + 16 * wave) >> shift;
+    const int j = own_place(step + TEAMS * lane) >> shift;
     return table[j < last_page ? j : last_page];
   };
   int pages = pages_from(begin + team);
@@ -109,7 +123,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   };
   auto load = [&](int step) {
     const int page = page_of(step);
-    const int in = (real(step) * kTokens + 16 * wave) & mask;
+    const int in = own_place(step) & mask;
     const int64_t page_head = ((int64_t)page * a.c.kv_heads + kvh) * ((int64_t)D << shift);
     const uint16_t* k = a.k_pages + page_head + in * D;
     const uint16_t* v = a.v_pages + page_head + in;
@@ -136,7 +150,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   auto fetch = [&](int step) {
     const int lane = apart(this_lane);
     const int page = page_of(step);
-    const int in = (real(step) * kTokens + 16 * wave) & mask;
+    const int in = own_place(step) & mask;
     const int64_t head = (int64_t)page * a.c.kv_heads + kvh;
     const uint8_t* k = reinterpret_cast<const uint8_t*>(a.k_pages) + (head * D << shift) + in * D;
     const uint8_t* v = reinterpret_cast<const uint8_t*>(a.v_pages) + (head * D << shift) + in;
@@ -157,9 +171,9 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   };
   auto store = [&](int step) {
     const int lane = apart(this_lane);
-    const int first = real(step) * kTokens;
-    if (first + kTokens > len || (first < first_seen && first + kTokens > a.sinks)) {
-      const int at = apart(first + 16 * wave);
+    const int step_at = place(kOfStep * step);
+    if (step_at + kTokens > len || (step_at < first_seen && step_at + kTokens > a.sinks)) {
+      const int at = apart(step_at + 16 * wave);
       auto seen = [&](int t) { return t < len && (t < a.sinks || t >= first_seen); };
       u32x4 keep = {0, 0, 0, 0};
       bool any = false;
@@ -257,7 +271,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   };
   // The same of the wave's own tokens that no row sees, whatever they are, before anybody reads them.
   auto clear_unseen = [&](int step) {
-    const int lane = apart(this_lane), at0 = real(step) * kTokens + 16 * wave;
+    const int lane = apart(this_lane), at0 = own_place(step);
     u32x4* vt = values_in_lds(step) + wave * (kHalf / kWaves / 16);
 #pragma unroll
     for (int n = 0; n < kHalf / kWaves / 16; n += 64) {
@@ -307,18 +321,19 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     };
     if (!known || !masked) v_batch(0);   // under way while the weights are made
     __builtin_amdgcn_s_setprio(0);
-    if (masked) {   // tokens of the lane up to `rel` are attended
+    if (masked) {
       if constexpr (WINDOW) {
         // Bit i of a word: the lane sees its token i; a logit's bit, spread over a word, keeps it or not (with compares and selects, some 60
-        // instructions more, nine prompts of up to 2,500, heads of 96, window 333 take 80.7 us, 77.4 so; 61 tokens 7.1 and 6.9).
-        const int first = real(step) * kTokens + (apart(this_lane) >> 5 << 3), rel = apart(pos) - first;
+        // instructions more, nine prompts of up to 2,500, heads of 96, window 333 took 80.7 us, 77.4 so; 61 tokens 7.1 and 6.9).
+        const int first = half_place(step, 0) + (apart(this_lane) >> 5 << 3), rel = apart(pos) - first;
         const int sinks = a.sinks - first, in = sinks < rel + 1 ? sinks : rel + 1;
         auto below = [](int n) { return n > 31 ? ~0u : (1u << (n > 0 ? n : 0)) - 1; };
         // (The wait is what has to lie between a matrix instruction and a read of its result: the compiler does not look into the two instructions below.)
         asm volatile("s_nop 15\n\ts_nop 7" : "+v"(x[0]), "+v"(x[1]));
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const uint32_t seen = (below(rel + 1 - 32 * t) & ~below(rel + 1 - a.window - 32 * t)) | below(in - 32 * t);
+          const int on = t * (half_place(step, 1) - half_place(step, 0));
+          const uint32_t seen = (below(rel + 1 - on) & ~below(rel + 1 - a.window - on)) | below(in - on);
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
             uint32_t keep;
@@ -326,7 +341,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
           }
         }
       } else {
-        const int rel = pos - real(step) * kTokens - 8 * half;
+        const int rel = pos - step * kTokens - 8 * half;   // tokens of the lane up to here are attended
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -366,7 +381,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
       for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
-          u32x4 f = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32) & up_to_last(real(step) * kTokens + 16 * c);
+          u32x4 f = *reinterpret_cast<const u32x4*>(v_at + (c * D + 32 * i) * 32) & up_to_last(step * kTokens + 16 * c);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t odd = odd_halves<BF16>(f[j]);
@@ -402,7 +417,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
       lds_written();
     } else {
       if constexpr (WINDOW) {
-        const int at = real(step) * kTokens + 16 * wave;
+        const int at = own_place(step);
         if (step < steps && (at + 16 > len || (at < first_seen && at + 16 > a.sinks))) {
           lds_arrived();
           clear_unseen(step);
@@ -416,9 +431,9 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     // Steps whose tokens all of the wave's rows attend, and others with a token that one of them does.
     for (; step - team < steps; step += TEAMS) {
       turn(step);
-      const int at = real(step) * kTokens, end = at + kTokens - 1;
+      const int at = half_place(step, 0), end = half_place(step, 1) + 31;   // (the step with the last sinks and the window's first tokens is one with a mask)
       if ((TEAMS == 1 || step < steps) && at <= wave_last && (end > wave_first - a.window || at < a.sinks))
-        work(step, !(end <= wave_first && (at > wave_last - a.window || end < a.sinks)));
+        work(step, !(end - at < kTokens && end <= wave_first && (at > wave_last - a.window || end < a.sinks)));
       if constexpr (E4M3) next_step(step);
     }
   } else {
@@ -455,7 +470,7 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     // 4,096 for NaN: no more than 16 of each in a sum.  (4,096 tokens x 32 heads of 128 whose values are all NaN: 1.7 ms, 0.17 with none.)
     constexpr uint32_t kExp = BF16 ? 0x7f80 : 0x7c00, kOne = BF16 ? 0x3f80 : 0x3c00, k64 = BF16 ? 0x4280 : 0x5400, k4096 = BF16 ? 0x4580 : 0x6c00;
     for (int gone = (begin + team) * kTokens; gone < steps * kTokens; gone += gone % kTokens ? 32 + (TEAMS - 1) * kTokens : 32) {
-      const int at = real(gone / kTokens) * kTokens + gone % kTokens;
+      const int at = place(gone / kGrain) + gone % kGrain;
       if (at > wave_last) break;
       int64_t head[2], block[2];   // of the 16 tokens' page; their scales
       u32x4 keep[2];

@@ -98,13 +98,14 @@ hipError_t launch_attn_prompt(const PromptArgs& d, int head_dim, bool, hipStream
     const int last = some_length(a.c.max_len) - 1;
     if (last < 0) continue;
     const int first_row = last - (int)(rng() % (unsigned)p.tokens);
-    int skip = 0;
+    int all = last / kPromptTokens + 1;
     if (a.window) {
       const int first = first_row - a.window + 1 > 0 ? first_row - a.window + 1 : 0;
-      const int sinks = a.sinks < first ? (a.sinks + kPromptTokens - 1) / kPromptTokens : first / kPromptTokens;
-      skip = first / kPromptTokens - sinks > 0 ? first / kPromptTokens - sinks : 0;
+      const int over = first / kPromptTokens - (a.sinks + kPromptTokens - 1) / kPromptTokens;   // in whole steps
+      if (over > 0) all -= over;
+      const int fine = first / 16 - (a.sinks + 31) / 32 * 2;                                     // in sixteens, pages in 16 bits
+      if (!a.k_scales && fine > 0 && (last / 16 - fine) / 4 + 1 < all) all = (last / 16 - fine) / 4 + 1;
     }
-    const int all = last / kPromptTokens + 1 - skip;
     REQUIRE(all >= 1 && (int64_t)p.steps * p.parts >= all);
   }
   if (p.parts > 1) {
