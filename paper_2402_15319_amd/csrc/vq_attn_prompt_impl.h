@@ -254,13 +254,15 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
   };
 
   // 16 bits, WINDOW: takes out of the step's values in LDS what is no number.  Another wave that is at the same does the same; one whose rows all see the
-  // step may read it before or after, and finds the word of it behind its last step.
+  // step may read it before or after, and finds the word of it behind its last step: a wave's own LDS operations are carried out in order, and the two
+  // asm statements with "words" keep the compiler to it, here (the word before any value) and there (the words behind all values).
   auto values_in_lds = [&](int step) {
     return reinterpret_cast<u32x4*>(lds + (2 * team + ((step / TEAMS) & 1)) * kStep + kHalf) + apart(this_lane);
   };
   auto clear_odd = [&](int step) {
     u32x4* vt = values_in_lds(step);
     odd_values[number] = 1;
+    asm volatile("; words: written" ::: "memory");
 #pragma unroll 1
     for (int n = 0; n < kHalf / 16; n += 64) {
       u32x4 v = vt[n];
@@ -458,8 +460,11 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) largest = __builtin_elementwise_maximum(largest, o[i][j]);   // NaN where one of them is
   if constexpr (WINDOW) {
+    asm volatile("; words: read" ::: "memory");
+    if (begin < steps) {   // (no step, no barrier behind the words' first values)
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) left_out |= odd_values[kWaves * team + i];
+      for (int i = 0; i < kWaves; ++i) left_out |= odd_values[kWaves * team + i];
+    }
   }
   if (__builtin_expect(__any(left_out != 0 || (__builtin_isunordered(largest, largest) && !__builtin_isunordered(l, l))), 0)) {
 #pragma unroll
