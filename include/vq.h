@@ -301,7 +301,7 @@ typedef struct vq_attn_desc {
   int32_t dtype;        /* VQ_F16 or VQ_BF16: q, k, v, out, and the cache if cache_dtype is 0 */
   float scale;          /* of the logits: positive, at most 2.35e38 (scale * log2(e) is
                            finite), as 1 / sqrt(head_dim)                             */
-  union {
+  __extension__ union {   /* (strict C99 takes it so) */
     int32_t cache_dtype;  /* 0: the pages hold values of dtype; VQ_E4M3: 8-bit codes with scales, below */
     int32_t reserved;     /* its name where it has to be 0                            */
   };
