@@ -289,7 +289,7 @@ VQ_API int vq_em_update(const vq_desc* desc, const void* W_f32, const void* hdia
  *     out = sum exp(t_j - m) v_j / l           lse = m + ln l
  * A row without any token to attend (p < 0) has out = 0 and lse = -infinity.  Query head h reads
  * key/value head h / (heads / kv_heads).  Products are accumulated, and m, l and the sums held, in
- * fp32; exp(t_j - m) is rounded to the cache's type for the second product, out once at the end.  Values that
+ * fp32; exp(t_j - m) is rounded to dtype for the second product (over pages in 8 bits too), out once at the end.  Values that
  * are no numbers go through the formula all the same: a weight that rounds to 0 still makes infinity of an infinite v.
  */
 typedef struct vq_attn_desc {
@@ -358,7 +358,8 @@ VQ_API int vq_cache_bytes(const vq_attn_desc* desc, size_t* bytes);
  * The new tokens' keys and values into their pages, copied bit for bit (pages in 8 bits: rounded as above); k and v are
  * [n_tokens][kv_heads][head_dim] with the strides given.  Tokens with a negative position, with one
  * of max_len or more, or in a page outside the cache, are left out.  k_pages and v_pages are 16-byte aligned; the arrays do
- * not overlap.  desc->scale is not used.  One launch.
+ * not overlap.  No two sequences of a call have new tokens in one page; a page in 8 bits that gets some
+ * changes for every sequence that lists it, earlier tokens too (a block's scale may grow).  desc->scale is not used.  One launch.
  */
 VQ_API int vq_cache_append(const vq_attn_desc* desc, const vq_attn_batch* batch,
                            const void* k, const vq_strides* k_strides,

@@ -179,7 +179,8 @@ class PagedCache:
 
     # ------------------------------------------------------------------ calls
     def batch(self, sequences, new=None) -> AttnBatch:
-        """The AttnBatch of these sequences with new[i] new tokens each, which their lengths already count (None: one each)."""
+        """The AttnBatch of these sequences with new[i] new tokens each, which their lengths already count (None: one each).  For
+        vq_cache_append each sequence is named once."""
         sequences = list(sequences)
         lens = [self._length[s] for s in sequences]
         width = max([1] + [len(self._pages[s]) for s in sequences])

@@ -56,7 +56,7 @@ struct DecodePlan {
   int32_t chunk, parts;   // tokens of a part; parts of the longest sequence
   int32_t tiles, cols;    // tiles of a key/value head's query heads; query heads of a tile at most
   int32_t together;       // tiles of a workgroup: 1, 2 or 3
-  int32_t waves;          // of a workgroup: 4 or 8; each takes 32 tokens in turn
+  int32_t waves;          // of a workgroup: 4 or 8; each takes 32 tokens in turn, 64 of pages in 8 bits
 };
 constexpr int kJoinCounters = 16384;   // at the start of the workspace: parts that have finished, zero between calls
 constexpr int kTileHeads = 16, kTogetherDim = 128;   // several tiles up to this head_dim: two of larger ones do not fit the registers (three of 128 spill 80 bytes)

@@ -4,7 +4,7 @@
 namespace vq {
 namespace {
 
-// 4,096 tokens x 32 heads of 128: 163 us, 845 TFLOP/s, 42 % of the matrix units' time, and 4 to 5 % behind 16 bits, whose K and V go to LDS past the registers:
+// 4,096 tokens x 32 heads of 128: 160 to 168 us by the card, 845 TFLOP/s at 163, 42 % of the matrix units' time, and 4 to 7 % behind 16 bits, whose K and V go to LDS past the registers:
 // codes stored before a step's products 180 us, behind them 179, and from places that are kept and without bank conflicts 163 to 168.
 template <bool BF16, int D, int TEAMS>
 __global__ __launch_bounds__(64 * kWaves * TEAMS, D == 256 ? 1 : 2) void prompt8_kernel(const PromptArgs A) {

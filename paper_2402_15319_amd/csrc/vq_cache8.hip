@@ -161,10 +161,10 @@ __global__ __launch_bounds__(256) void append8_few_kernel(const AppendArgs a) {
 // eight dimensions in registers.  Where the source runs along positions a wave takes all of them and 64 dimensions, otherwise all dimensions of as many positions
 // as it has lanes for.  The lanes, and in the first case the waves, that have a block exchange their largest magnitudes.  Loads are 16 bytes along whatever is
 // contiguous in the source, 128 or more in a row of lanes; the lane turns its block where the page runs along the other; values' codes of whole blocks
-// go through LDS to the lane that stores a dimension's 16 at once, successive dimensions in successive lanes.  Memory bounds it (11,700 tokens x 32 heads of
-// 128, pages of 16, 287 MB: rows whole 61 us, 4.7 TB/s, and 67 with values stored 8 bytes by 8 from where they are; a conversion of as many bytes in order 51.  In
-// the order of the batched product 76, 64 where sequences begin at multiples of 64 in the source and in the page: lines are read in two halves otherwise, and odd
-// numbers cost 16-byte loads their alignment).  8 waves to a SIMD, loads past the caches (85 us) or stores past them do no better.  16 positions in place of 64 (a
+// go through LDS to the lane that stores a dimension's 16 at once, successive dimensions in successive lanes.  Memory bounds it where rows are whole (11,700 tokens x 32
+// heads of 128, pages of 16, 287 MB: 61 us, 4.7 TB/s, and 67 with values stored 8 bytes by 8 from where they are; a conversion of as many bytes in order 51).  In
+// the order of the batched product the loads do, 77 us with no more traffic (201 MB read, 98 written) and 62 where sequences begin at multiples of 64 in the source and in
+// the page: otherwise lines are read in two halves, and odd numbers cost 16-byte loads their alignment.  8 waves to a SIMD, loads past the caches (85 us) or stores past them do no better.  16 positions in place of 64 (a
 // block to a lane) reads half lines: 44 us for 32 tokens of one sequence, 6 with 64.
 constexpr int kTile8 = 64;
 template <bool BF16, int D>
@@ -314,7 +314,10 @@ template <bool BF16, int D>
 hipError_t launch_dim(const AppendArgs& a, hipStream_t s) {
   // Few new tokens for each sequence: most of a tile would be empty, but each of them goes through the block's others.  (64 sequences x 32 heads of 128, rows
   // whole: one new token each 5.7 us, 13.0 in tiles; four 16.3 and 14.0.  In the order of the batched product: one 8.4 and 18.8; two 14.6 and 19.8; three 27.5
-  // and 21.7.  512 sequences x 8 heads, rows whole: four 28.5 and 35.8; in the order of the product two 23.7 and 49.5, four 69.7 and 52.6.)
+  // and 21.7.  512 sequences x 8 heads, rows whole: four 28.5 and 35.8; in the order of the product two 23.7 and 49.5, four 69.7 and 52.6.)  The host knows their mean
+  // alone, so these lines are for sequences with about as many each: a chunk among single tokens goes token by token too (64 behind 63 of them, 8 heads, rows whole: 13.7 us,
+  // 6.9 in tiles, in the order of the product 20.2 and 9.3; 32 heads 22.2 and 12.5, 47.1 and 17.9; 512 behind 511, 8 heads: 27.1 and 36.3, 75.2 and 55.7).  Where that
+  // counts, the chunk is better appended by a call of its own.
   const int few = a.ks.dim == 1 && a.vs.dim == 1 ? 3 : 2;
   if (!a.c.q_start || a.c.n_tokens <= few * (int64_t)a.c.n_seqs)
     append8_few_kernel<BF16, D><<<dim3(a.c.n_tokens, (a.c.kv_heads * octets(D) + 255) / 256), 256, 0, s>>>(a);
