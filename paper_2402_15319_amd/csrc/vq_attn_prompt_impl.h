@@ -577,13 +577,16 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
     const float old = m;
     m = fmaxf(m, ml[0]);
     const float base = m == -INFINITY ? 0.f : m, f0 = rescale(old, base), f1 = rescale(ml[0], base);
-    l = f0 * l + f1 * ml[1];
+    // Here and below one of two products is fused with the sum, as written: a build that chooses changes the last bits.  (Which one it is calls have had since
+    // there are teams and parts.)
+    l = fmaf(f0, l, f1 * ml[1]);
 #pragma unroll
     for (int i = 0; i < 4 * DT; ++i) {
       const f32x4 v = at[(1 + i) * 64];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        o[i >> 2][4 * (i & 3) + j] = f0 * o[i >> 2][4 * (i & 3) + j] + f1 * v[j];
+        const float first = o[i >> 2][4 * (i & 3) + j];
+        o[i >> 2][4 * (i & 3) + j] = !WINDOW || i < 6 ? fmaf(f1, v[j], f0 * first) : fmaf(f0, first, f1 * v[j]);
       }
     }
   }
@@ -634,14 +637,14 @@ __device__ __forceinline__ void prompt_body(const PromptArgs& A) {
           old = rescale(m, base);
           now = rescale(ml[0], base);
           m = top;
-          l = old * l + now * ml[1];
+          l = fmaf(old, l, now * ml[1]);
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int d = 2 * (at + j) + e;
-            o[d >> 4][d & 15] = old * o[d >> 4][d & 15] + now * v[j][e];
+            o[d >> 4][d & 15] = !WINDOW && (D == 64 || D == 256) ? fmaf(now, v[j][e], old * o[d >> 4][d & 15]) : fmaf(old, o[d >> 4][d & 15], now * v[j][e]);
           }
         __builtin_amdgcn_sched_barrier(0);
       }
