@@ -375,12 +375,6 @@ def _rows(t, n: int, heads: int, dim: int, what: str, kind, gpu: int):
     return None if t.is_contiguous() else VQStrides(*t.stride())
 
 
-def _whole(desc: VQAttnDesc):
-    """Bytes and type of a K or V buffer."""
-    n = desc.n_pages * desc.kv_heads * desc.page_size
-    return (n * desc.head_dim + n // 4, _kinds.get(VQ_E4M3)) if desc.cache_dtype else (2 * n * desc.head_dim, _kinds.get(desc.dtype))
-
-
 def _pages(t, size: int, what: str, kind, gpu: int) -> int:
     """The address of a K or V buffer (an address passes through)."""
     try:
@@ -401,7 +395,8 @@ def vq_cache_bytes(desc: VQAttnDesc) -> int:
 def vq_cache_append(desc: VQAttnDesc, batch: AttnBatch, k, v, k_pages, v_pages, stream=None) -> None:
     """k, v: [n_tokens, kv_heads, head_dim] views (strides as vq_strides allows) of the new tokens."""
     n, heads, dim, kind, gpu = batch.n_tokens, desc.kv_heads, desc.head_dim, _kinds.get(desc.dtype), batch.gpu
-    size, held = _whole(desc)
+    slots = desc.n_pages * heads * desc.page_size
+    size, held = (slots * dim + slots // 4, _kinds.get(VQ_E4M3)) if desc.cache_dtype else (2 * slots * dim, kind)
     _check(lib().vq_cache_append(desc, batch.struct, k.data_ptr(), _rows(k, n, heads, dim, "k", kind, gpu), v.data_ptr(),
                                  _rows(v, n, heads, dim, "v", kind, gpu), _pages(k_pages, size, "k_pages", held, gpu),
                                  _pages(v_pages, size, "v_pages", held, gpu), _stream(stream)), "vq_cache_append")
@@ -436,14 +431,15 @@ def attn_workspace(desc: VQAttnDesc, batch: AttnBatch, device=None):
     return torch.zeros(vq_attn_workspace_bytes(desc, batch), dtype=torch.uint8, device=batch.device if device is None else device)
 
 
-def _attn(call, name, desc, batch, q, k_pages, v_pages, out, workspace, lse, stream, *window):
+def _attn(call, name, desc, batch, q, k_pages, v_pages, out, workspace, lse, stream):
     n, heads, dim, kind, gpu = batch.n_tokens, desc.heads, desc.head_dim, _kinds.get(desc.dtype), batch.gpu
-    size, held = _whole(desc)
+    slots = desc.n_pages * desc.kv_heads * desc.page_size
+    size, held = (slots * dim + slots // 4, _kinds.get(VQ_E4M3)) if desc.cache_dtype else (2 * slots * dim, kind)
     if lse is not None and (lse.shape != (n, heads) or lse.dtype is not _kinds[VQ_F32] or not lse.is_contiguous() or lse.get_device() != gpu):
         raise ValueError(f"{name}: lse is a contiguous float32 tensor [n_tokens, heads] on the batch's GPU")
     if workspace.get_device() != gpu:
         raise ValueError(f"{name}: the workspace is on the batch's GPU")
-    _check(call(desc, batch.struct, *window, q.data_ptr(), _rows(q, n, heads, dim, "q", kind, gpu), _pages(k_pages, size, "k_pages", held, gpu),
+    _check(call(desc, batch.struct, q.data_ptr(), _rows(q, n, heads, dim, "q", kind, gpu), _pages(k_pages, size, "k_pages", held, gpu),
                 _pages(v_pages, size, "v_pages", held, gpu), out.data_ptr(), _rows(out, n, heads, dim, "out", kind, gpu), _ptr(lse),
                 _ptr(workspace), workspace.nbytes, _stream(stream)), name)
 
@@ -460,9 +456,11 @@ def vq_attn_prompt(desc: VQAttnDesc, batch: AttnBatch, q, k_pages, v_pages, out,
 
 def vq_attn_decode_window(desc: VQAttnDesc, batch: AttnBatch, window: VQAttnWindow, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:
     """vq_attn_decode of the window's tokens and the first ones that stay visible."""
-    _attn(lib().vq_attn_decode_window, "vq_attn_decode_window", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream, window)
+    call = lib().vq_attn_decode_window
+    _attn(lambda d, b, *rest: call(d, b, window, *rest), "vq_attn_decode_window", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream)
 
 
 def vq_attn_prompt_window(desc: VQAttnDesc, batch: AttnBatch, window: VQAttnWindow, q, k_pages, v_pages, out, workspace, lse=None, stream=None) -> None:
     """vq_attn_prompt of each token's window and the first ones that stay visible."""
-    _attn(lib().vq_attn_prompt_window, "vq_attn_prompt_window", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream, window)
+    call = lib().vq_attn_prompt_window
+    _attn(lambda d, b, *rest: call(d, b, window, *rest), "vq_attn_prompt_window", desc, batch, q, k_pages, v_pages, out, workspace, lse, stream)
