@@ -59,7 +59,7 @@ struct DecodePlan {
   int32_t waves;          // of a workgroup: 4 or 8; each takes 32 tokens in turn, 64 of pages in 8 bits
 };
 constexpr int kJoinCounters = 16384;   // at the start of the workspace: parts that have finished, zero between calls
-constexpr int kTileHeads = 16, kTogetherDim = 128;   // several tiles up to this head_dim: two of larger ones do not fit the registers (three of 128 spill 80 bytes)
+constexpr int kTileHeads = 16, kTogetherDim = 128;   // several tiles up to this head_dim: two of larger ones do not fit the registers (three of 128 spill 76 bytes)
 constexpr int kThreeDim8 = 64;         // three tiles in 8 bits up to this head_dim: of 96 and 128 they spill 36 and 252 bytes
 constexpr int kMostParts = 64;         // of a sequence
 
